@@ -284,6 +284,159 @@ int agg_global_attn_fwd_list(const agg_shape* shape, int64_t M_list, const void*
                              const float* vmean, const uint32_t* kept_bits,
                              const int32_t* n_dropped, void* O, float* lse, void* hip_stream);
 
+/*
+ * ---- The other parts of a model's block ----
+ * What the models around these attention layers put between projections and attention, and between
+ * one block and the next.  Statistics, angles and sums are float32 or better; every output is rounded
+ * to bf16 once.  As for every call, the device that holds the tensors must be the current one.
+ */
+enum {
+  AGG_NORM_NONE = 0,  /* y = x                                                          */
+  AGG_NORM_LAYER = 1, /* y = (x - mean) / sqrt(var + eps) * gamma + beta                */
+  AGG_NORM_RMS = 2    /* y = x / sqrt(mean(x^2) + eps) * gamma + beta                   */
+};
+typedef struct agg_norm {
+  int32_t kind;       /* AGG_NORM_*; NONE: the other fields are ignored                 */
+  float eps;          /* > 0                                                            */
+  const float* gamma; /* device float32, one per channel, 16-byte aligned; NULL: ones   */
+  const float* beta;  /* ... NULL: zeros                                                */
+} agg_norm;
+
+/*
+ * Rotary positions on three axes.  d_t, d_h, d_w channels of every head turn with the token's time,
+ * row and column (each even, together at most D, 0 leaves an axis out); the channels behind them are
+ * left as they are.  A pair (x, y) at position p of its axis becomes
+ *     (x cos a - y sin a, y cos a + x sin a),   a = p * base^-e:
+ *   SECTIONS    an axis's d channels follow each other from channel s; pairs (s+j, s+j+d/2), e = 2j/d
+ *   NEIGHBOURS  the same, pairs (s+2j, s+2j+1), e = 2j/d
+ *   HEAD        r = d_t+d_h+d_w; pairs (i, i+r/2), e = 2i/r, the first d_t/2 pairs turn with time, the
+ *               next d_h/2 with the row, the rest with the column
+ * Positions: `pos`, device int32 [B, N*L, 3] (time, row, column), any values; or pos = NULL, the
+ * token's place in the sequence: time t0 + frame, row and column counted from patch0 for patches and
+ * 0 for special tokens.  a is reduced to one turn in 64-bit integers, so that far positions lose
+ * nothing.
+ */
+enum { AGG_ROPE_SECTIONS = 0, AGG_ROPE_NEIGHBOURS = 1, AGG_ROPE_HEAD = 2 };
+typedef struct agg_rope {
+  int32_t pairing;       /* AGG_ROPE_* */
+  int32_t d_t, d_h, d_w;
+  int32_t t0;            /* time of frame 0; t0 + N may not pass 2^31 - 1 */
+  int32_t patch0;        /* row and column of a frame's first patch       */
+  float base;            /* >= 1, finite                                  */
+} agg_rope;
+
+/*
+ * Qr = turn(norm(Q)), Kr = turn(norm(K)), head by head: what belongs between the Q/K projections and
+ * any of the attention calls.  q_norm, k_norm over a head's D channels (NULL: none); rope NULL: no
+ * rotation.  Q, K: device bf16, token t of batch element b at element (b*N*L + t) * stride, stride 0
+ * meaning H*D (contiguous), otherwise a multiple of 8 and >= H*D: a fused projection's output is read
+ * where it is.  Qr, Kr: [B, N*L, H, D], contiguous.  Qr = Q and Kr = K (contiguous) work in place;
+ * other overlaps of an output with an input or the other output are refused with AGG_ERR_SHAPE.  Q and Qr may both be
+ * NULL, or K and Kr.  Of `shape` only B, N, n_h, n_w, n_special, H and D matter.
+ */
+int agg_rope_fwd(const agg_shape* shape, const agg_rope* rope, const agg_norm* q_norm,
+                 const agg_norm* k_norm, const int32_t* pos, const void* Q, int64_t q_stride,
+                 const void* K, int64_t k_stride, void* Qr, void* Kr, void* hip_stream);
+
+/*
+ * The seam between a branch (attention, token-wise network) and the next one:
+ *     h = x + gate * scale * post(branch),     n = pre(h)
+ * post: the norm behind the branch, pre: the norm in front of the next branch (of the unrounded h).
+ * x, branch, h, n: device bf16 [rows, C].  scale: device float32 [C], 16-byte aligned (NULL: ones).  gate: device bf16
+ * [ceil(rows / gate_rows), C], row r uses gate[r / gate_rows] (NULL: ones; gate_rows is then
+ * ignored).  branch NULL: h = x.  h may be NULL (not written); n must be given exactly if pre.kind
+ * is not NONE.  h = x, h = branch, n = x and n = branch work in place; other overlaps of outputs with x, branch, gate or each
+ * other are refused with AGG_ERR_SHAPE.  C: a multiple of 8, at most 8192 (AGG_ERR_UNSUPPORTED).  rows = 0: nothing is done.
+ */
+typedef struct agg_residual {
+  agg_norm post, pre;
+  const float* scale;
+  const void* gate;
+  int64_t gate_rows;
+} agg_residual;
+int agg_residual_norm_fwd(int64_t rows, int32_t C, const agg_residual* residual, const void* x,
+                          const void* branch, void* h, void* n, void* hip_stream);
+
+/*
+ * ---- Microscaled 4-bit floats ----
+ * A matrix [rows, K] in 4 bits: 32 consecutive channels of a row share a scale 2^(s - 127), s one
+ * byte; each channel holds a 4-bit float, sign + one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (codes 0..7, sign
+ * in bit 3).  s = 255 makes the 32 values NaN.
+ *   codes   [rows, agg_mx4_code_stride(K)] bytes, channel k in byte k/2, low half if k is even
+ *   scales  [rows, agg_mx4_scale_stride(K)] bytes, channel k's in byte k/32
+ * The strides are K/2 rounded up to 128 and K/32 rounded up to 16, so that rows begin on whole lines;
+ * the bytes behind a row's end (and the codes behind K in the last byte run) must be 0, as
+ * agg_mx4_quantize leaves them.  Codes and scales are 16-byte aligned.
+ *
+ * Quantisation: s - 127 = floor(log2(largest magnitude)) - 2, at least -127 (all zeros: s = 0); values
+ * are divided by the scale and rounded to the nearest 4-bit float, ties to the even code, magnitudes
+ * above 6 to 6.  A block with a NaN or infinity gets s = 255 and codes 0.
+ */
+int64_t agg_mx4_code_stride(int32_t K);  /* host only; 0 for K < 1 */
+int64_t agg_mx4_scale_stride(int32_t K);
+
+/* x: device bf16, row r at element r * x_stride (0: K); K and x_stride multiples of 8.  rows = 0: nothing is done. */
+int agg_mx4_quantize(int64_t rows, int32_t K, const void* x, int64_t x_stride, void* codes,
+                     void* scales, void* hip_stream);
+
+/* The values that codes and scales stand for, as bf16 [rows, K] (exact; above the type's range
+ * infinite).  K a multiple of 8. */
+int agg_mx4_dequantize(int64_t rows, int32_t K, const void* codes, const void* scales, void* x,
+                       void* hip_stream);
+
+/*
+ * Y_i = A W_i^T + bias_i for i < count (1..3, one launch), or with a residual (count = 1)
+ *     Y = R + res_scale * (A W^T + bias)
+ * A: [rows, K] and W_i: [N, K] in 4 bits; products and sums in float32, one rounding.  bias_i: float32
+ * [N], 16-byte aligned, or NULL.  Y_i, R: bf16 [rows, N], contiguous; Y = R works in place, other overlaps of outputs with R or each other are
+ * refused with AGG_ERR_SHAPE.  res_scale: like bias_i (NULL: ones; must be NULL without R).
+ * K and N are multiples of 8.  A row's bits do not depend on the other rows of the call, but on which
+ * kernel its number of rows leads to.  rows = 0: nothing is done.
+ */
+typedef struct agg_mx4_matrix {
+  const void* codes;
+  const void* scales;
+} agg_mx4_matrix;
+typedef struct agg_mx4_linear {
+  int32_t count;
+  agg_mx4_matrix w[3];
+  const float* bias[3];
+  void* y[3];
+  const void* residual;
+  const float* res_scale;
+} agg_mx4_linear;
+int agg_mx4_linear_fwd(int64_t rows, int32_t N, int32_t K, const agg_mx4_linear* linear,
+                       const void* codes, const void* scales, void* hip_stream);
+
+/*
+ * agg_global_block_fwd with the parts above:
+ *     [Q|K|V] = W_{q,k,v} first(x) + b_{q,k,v},  Q = turn(q_norm(Q)),  K = turn(k_norm(K)),
+ *     y = x + gate * scale * post(W_o Attn(Q, K, V) + b_o),   n = pre(y)
+ * weights: as in agg_global_block_fwd, its LayerNorm being `first` (skipped if first_done: x_norm
+ * then holds first(x), the n of the block before).  With mx (all four matrices) the projections are
+ * products of 4-bit floats: their inputs are quantised, and w_q .. w_o are not read (may be NULL).
+ * Everything that is zero or NULL in the options is left out; with all of it left out the result
+ * is that of agg_global_block_fwd.  With a norm, a gate or (bf16 weights) a scale behind the output
+ * projection, its result is rounded to bf16 before them, as every tensor between the parts is.
+ * n: bf16 [B, N*L, C], exactly if residual.pre.kind is not NONE.  y, n, x and x_norm may not overlap, save n = x_norm.
+ */
+typedef struct agg_block_options {
+  const agg_rope* rope;
+  const int32_t* pos;
+  agg_norm q_norm, k_norm;
+  agg_residual residual;
+  int32_t first_done;
+  const void* x_norm;
+  const agg_mx4_matrix* mx; /* host array of 4: q, k, v, o; NULL: the bf16 weights */
+} agg_block_options;
+
+/* Host only.  Scratch bytes agg_global_block_ex_fwd needs (0 on an invalid shape). */
+size_t agg_block_ex_workspace_bytes(const agg_shape* shape, int mode, const agg_block_options* options);
+
+int agg_global_block_ex_fwd(const agg_shape* shape, int mode, const agg_block_weights* weights,
+                            const agg_block_options* options, const void* x, void* y, void* n,
+                            void* workspace, size_t workspace_bytes, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -68,6 +68,9 @@ EXPORTS = [
     "agg_select_kv_indices", "agg_list_compact_bytes", "agg_list_workspace_bytes",
     "agg_kv_subsample_list", "agg_global_attn_fwd_list", "agg_kv_pool",
     "agg_static_scratch_bytes", "agg_kv_subsample_static",
+    "agg_rope_fwd", "agg_residual_norm_fwd",
+    "agg_mx4_code_stride", "agg_mx4_scale_stride", "agg_mx4_quantize", "agg_mx4_dequantize",
+    "agg_mx4_linear_fwd", "agg_block_ex_workspace_bytes", "agg_global_block_ex_fwd",
 ]
 
 AGG_SELECT_FIRST = 0
@@ -97,6 +100,103 @@ def make_block_weights(ln_gamma, ln_beta, ln_eps, w_q, w_k, w_v, w_o, b_q=None, 
         return None if t is None else t.data_ptr()
     return agg_block_weights(p(ln_gamma), p(ln_beta), float(ln_eps), p(w_q), p(w_k), p(w_v),
                              p(w_o), p(b_q), p(b_k), p(b_v), p(b_o))
+
+
+AGG_NORM_NONE = 0
+AGG_NORM_LAYER = 1
+AGG_NORM_RMS = 2
+
+AGG_ROPE_SECTIONS = 0
+AGG_ROPE_NEIGHBOURS = 1
+AGG_ROPE_HEAD = 2
+
+
+class agg_norm(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("eps", ctypes.c_float), ("gamma", ctypes.c_void_p),
+                ("beta", ctypes.c_void_p)]
+
+
+class agg_rope(ctypes.Structure):
+    _fields_ = [("pairing", ctypes.c_int32), ("d_t", ctypes.c_int32), ("d_h", ctypes.c_int32),
+                ("d_w", ctypes.c_int32), ("t0", ctypes.c_int32), ("patch0", ctypes.c_int32),
+                ("base", ctypes.c_float)]
+
+
+class agg_residual(ctypes.Structure):
+    _fields_ = [("post", agg_norm), ("pre", agg_norm), ("scale", ctypes.c_void_p),
+                ("gate", ctypes.c_void_p), ("gate_rows", ctypes.c_int64)]
+
+
+class agg_mx4_matrix(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
+
+
+class agg_mx4_linear(ctypes.Structure):
+    _fields_ = [("count", ctypes.c_int32), ("w", agg_mx4_matrix * 3), ("bias", ctypes.c_void_p * 3),
+                ("y", ctypes.c_void_p * 3), ("residual", ctypes.c_void_p), ("res_scale", ctypes.c_void_p)]
+
+
+class agg_block_options(ctypes.Structure):
+    _fields_ = [("rope", ctypes.POINTER(agg_rope)), ("pos", ctypes.c_void_p), ("q_norm", agg_norm),
+                ("k_norm", agg_norm), ("residual", agg_residual), ("first_done", ctypes.c_int32),
+                ("x_norm", ctypes.c_void_p), ("mx", ctypes.POINTER(agg_mx4_matrix))]
+
+
+# The structs below hold on to the tensors whose addresses they carry.
+def make_norm(kind=AGG_NORM_NONE, eps=1e-5, gamma=None, beta=None) -> agg_norm:
+    n = agg_norm(int(kind), float(eps), _ptr(gamma), _ptr(beta))
+    n.keep = (gamma, beta)
+    return n
+
+
+def make_rope(pairing, d_t, d_h, d_w, base=100.0, t0=0, patch0=0) -> agg_rope:
+    return agg_rope(int(pairing), int(d_t), int(d_h), int(d_w), int(t0), int(patch0), float(base))
+
+
+def make_residual(post=None, pre=None, scale=None, gate=None, gate_rows=0) -> agg_residual:
+    post, pre = post or agg_norm(), pre or agg_norm()
+    r = agg_residual(post, pre, _ptr(scale), _ptr(gate), int(gate_rows))
+    r.keep = (post, pre, scale, gate)
+    return r
+
+
+def make_mx4_linear(weights, outs, biases=None, residual=None, res_scale=None) -> agg_mx4_linear:
+    """weights: one to three (codes, scales), outs as many tensors, biases as many (None: none)."""
+    weights, outs = list(weights), list(outs)
+    biases = list(biases) if biases is not None else [None] * len(weights)
+    if not 1 <= len(weights) <= 3 or len(outs) != len(weights) or len(biases) != len(weights):
+        raise ValueError("one to three weights, and as many outputs and biases")
+    m = agg_mx4_linear()
+    m.count = len(weights)
+    for i, (codes, scales) in enumerate(weights):
+        m.w[i] = agg_mx4_matrix(_ptr(codes), _ptr(scales))
+        m.bias[i], m.y[i] = _ptr(biases[i]), _ptr(outs[i])
+    m.residual, m.res_scale = _ptr(residual), _ptr(res_scale)
+    m.keep = (weights, outs, biases, residual, res_scale)
+    return m
+
+
+def make_block_options(rope=None, pos=None, q_norm=None, k_norm=None, residual=None, x_norm=None,
+                       mx=None) -> agg_block_options:
+    """x_norm given: the first norm is done.  mx: (codes, scales) of the q, k, v and o matrices."""
+    o = agg_block_options()
+    if rope is not None:
+        o.rope = ctypes.pointer(rope)
+    o.pos = _ptr(pos)
+    for name, value in (("q_norm", q_norm), ("k_norm", k_norm), ("residual", residual)):
+        if value is not None:
+            setattr(o, name, value)
+    o.first_done, o.x_norm = int(x_norm is not None), _ptr(x_norm)
+    if mx is not None:
+        mx = list(mx)
+        if len(mx) != 4:
+            raise ValueError("four matrices: q, k, v, o")
+        held = (agg_mx4_matrix * 4)(*[agg_mx4_matrix(_ptr(c), _ptr(s)) for c, s in mx])
+        o.mx = ctypes.cast(held, ctypes.POINTER(agg_mx4_matrix))
+    else:
+        held = None
+    o.keep = (rope, pos, q_norm, k_norm, residual, x_norm, mx, held)
+    return o
 
 
 def lib():
@@ -149,6 +249,20 @@ def lib():
     L.agg_static_scratch_bytes.restype = ctypes.c_size_t
     L.agg_static_scratch_bytes.argtypes = []
     L.agg_kv_subsample_static.argtypes = [shp, vp, vp, vp, vp, vp, vp, vp, vp]
+    normp, i64 = ctypes.POINTER(agg_norm), ctypes.c_int64
+    L.agg_rope_fwd.argtypes = [shp, ctypes.POINTER(agg_rope), normp, normp, vp, vp, i64, vp, i64, vp, vp, vp]
+    L.agg_residual_norm_fwd.argtypes = [i64, ctypes.c_int32, ctypes.POINTER(agg_residual), vp, vp, vp, vp, vp]
+    for fn in (L.agg_mx4_code_stride, L.agg_mx4_scale_stride):
+        fn.restype, fn.argtypes = i64, [ctypes.c_int32]
+    L.agg_mx4_quantize.argtypes = [i64, ctypes.c_int32, vp, i64, vp, vp, vp]
+    L.agg_mx4_dequantize.argtypes = [i64, ctypes.c_int32, vp, vp, vp, vp]
+    L.agg_mx4_linear_fwd.argtypes = [i64, ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(agg_mx4_linear),
+                                     vp, vp, vp]
+    opts = ctypes.POINTER(agg_block_options)
+    L.agg_block_ex_workspace_bytes.restype = ctypes.c_size_t
+    L.agg_block_ex_workspace_bytes.argtypes = [shp, ctypes.c_int, opts]
+    L.agg_global_block_ex_fwd.argtypes = [shp, ctypes.c_int, ctypes.POINTER(agg_block_weights), opts, vp, vp, vp,
+                                          vp, ctypes.c_size_t, vp]
     global _raw_stream
     # the current stream's handle without building a Stream object for it (3 us a call)
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -324,3 +438,51 @@ def agg_global_attn_fwd_list(shape, M_list, Q, K, V, Kc, Vc, kmean, vmean, kept_
 def agg_kv_pool(shape, K, V, Kc, Vc, stream=None):
     _check(lib().agg_kv_pool(ctypes.byref(shape), _ptr(K), _ptr(V), _ptr(Kc), _ptr(Vc),
                              _stream(stream)), "agg_kv_pool")
+
+
+def _ref(struct):
+    return None if struct is None else ctypes.byref(struct)
+
+
+def agg_rope_fwd(shape, rope, q_norm, k_norm, pos, Q, q_stride, K, k_stride, Qr, Kr, stream=None):
+    _check(lib().agg_rope_fwd(ctypes.byref(shape), _ref(rope), _ref(q_norm), _ref(k_norm), _ptr(pos),
+                              _ptr(Q), int(q_stride), _ptr(K), int(k_stride), _ptr(Qr), _ptr(Kr),
+                              _stream(stream)), "agg_rope_fwd")
+
+
+def agg_residual_norm_fwd(rows, C, residual, x, branch, h, n, stream=None):
+    _check(lib().agg_residual_norm_fwd(int(rows), int(C), ctypes.byref(residual), _ptr(x), _ptr(branch),
+                                       _ptr(h), _ptr(n), _stream(stream)), "agg_residual_norm_fwd")
+
+
+def agg_mx4_code_stride(K: int) -> int:
+    return int(lib().agg_mx4_code_stride(int(K)))
+
+
+def agg_mx4_scale_stride(K: int) -> int:
+    return int(lib().agg_mx4_scale_stride(int(K)))
+
+
+def agg_mx4_quantize(rows, K, x, x_stride, codes, scales, stream=None):
+    _check(lib().agg_mx4_quantize(int(rows), int(K), _ptr(x), int(x_stride), _ptr(codes), _ptr(scales),
+                                  _stream(stream)), "agg_mx4_quantize")
+
+
+def agg_mx4_dequantize(rows, K, codes, scales, x, stream=None):
+    _check(lib().agg_mx4_dequantize(int(rows), int(K), _ptr(codes), _ptr(scales), _ptr(x),
+                                    _stream(stream)), "agg_mx4_dequantize")
+
+
+def agg_mx4_linear_fwd(rows, N, K, linear, codes, scales, stream=None):
+    _check(lib().agg_mx4_linear_fwd(int(rows), int(N), int(K), ctypes.byref(linear), _ptr(codes),
+                                    _ptr(scales), _stream(stream)), "agg_mx4_linear_fwd")
+
+
+def agg_block_ex_workspace_bytes(shape: agg_shape, mode: int, options: agg_block_options) -> int:
+    return int(lib().agg_block_ex_workspace_bytes(ctypes.byref(shape), int(mode), ctypes.byref(options)))
+
+
+def agg_global_block_ex_fwd(shape, mode, weights, options, x, y, n, workspace, workspace_bytes, stream=None):
+    _check(lib().agg_global_block_ex_fwd(ctypes.byref(shape), int(mode), ctypes.byref(weights),
+                                         ctypes.byref(options), _ptr(x), _ptr(y), _ptr(n), _ptr(workspace),
+                                         int(workspace_bytes), _stream(stream)), "agg_global_block_ex_fwd")

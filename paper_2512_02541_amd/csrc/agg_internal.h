@@ -155,6 +155,65 @@ struct LinearOuts {
 hipError_t launch_linear(const void* A, const LinearOuts& outs, const void* R, int64_t rows, int N,
                          int K, hipStream_t st);
 
+// Rotary positions behind a norm (agg_rope_fwd); [0]: queries, [1]: keys.
+struct SeamNorm {
+  int32_t kind;
+  float eps;
+  const float* gamma;
+  const float* beta;
+};
+struct RopeArgs {
+  const uint16_t* in[2];  // null: this tensor is left out
+  uint16_t* out[2];
+  int64_t stride[2];      // elements from a token's row of `in` to the next
+  SeamNorm norm[2];
+  const int32_t* pos;     // [tokens, 3], or null: from the token's place
+  int64_t total, NQ;      // tokens of all sequences, of one
+  int32_t H, L, P, n_w, t0, patch0;
+  int32_t pairs;          // pairs of channels that turn, 0: none
+  int32_t tokens;         // of a wavefront's turn (set by launch_rope)
+  uint64_t freq[kHeadDim / 2];     // of a pair, in 2^-64 turns per position
+  uint8_t axis[kHeadDim / 2];      // 0 time, 1 row, 2 column
+  // of a channel: its pair's other channel (bits 0..5), the pair (6..10), whether the other's share
+  // is added (11), whether it turns at all (12)
+  uint16_t channel[kHeadDim];
+};
+hipError_t launch_rope(const RopeArgs& args, hipStream_t st);
+
+// h = x + gate * scale * post(branch), n = pre(h) (agg_residual_norm_fwd)
+struct SeamArgs {
+  const uint16_t *x, *branch, *gate;
+  const float* scale;
+  uint16_t *h, *n;
+  SeamNorm post, pre;
+  int64_t rows, gate_rows;
+  int32_t C;
+};
+hipError_t launch_seam(const SeamArgs& args, hipStream_t st);
+
+// Matrices of microscaled 4-bit floats: bytes of a row of codes and of scales, whole 128-byte lines
+// and as many scales as two of them can need
+constexpr int64_t mx4_code_stride(int64_t K) { return (K + 255) / 256 * 128; }
+constexpr int64_t mx4_scale_stride(int64_t K) { return (K + 511) / 512 * 16; }
+hipError_t launch_mx4_quantize(const void* x, int64_t x_stride, void* codes, void* scales, int64_t rows, int K,
+                               hipStream_t st);
+hipError_t launch_mx4_dequantize(const void* codes, const void* scales, void* x, int64_t rows, int K, hipStream_t st);
+struct Mx4Matrix {
+  const uint8_t *codes, *scales;
+};
+struct Mx4LinearArgs {
+  Mx4Matrix a, w[3];
+  const float* bias[3];
+  uint16_t* y[3];
+  const uint16_t* residual;
+  const float* res_scale;
+  int64_t rows;
+  int32_t N, K, count;
+  int32_t code_stride, scale_stride;
+  int32_t gn;  // channel tiles of a matrix (set by launch_mx4_linear)
+};
+hipError_t launch_mx4_linear(const Mx4LinearArgs& args, hipStream_t st);
+
 int mean_chunks(const Geom& g);  // number of partial-sum blocks the mean kernel uses
 
 // Device array inside the library that stands in for the caller's workspace in

@@ -225,3 +225,64 @@ def pool_forward(shape, Q, K, V):
     agg.agg_kv_pool(plain, K, V, buf.Kc, buf.Vc)
     attend(buf, Q, K, V)
     return buf
+
+
+# ---- the other parts of a block -------------------------------------------------------------
+def rope_forward(shape, rope, Q, K, q_norm=None, k_norm=None, pos=None, q_stride=0, k_stride=0):
+    """Normalised and turned queries and keys [B, NQ, H, D]; Q or K may be None."""
+    full = (shape.B, shape.NQ, shape.H, shape.D)
+    out = [None if t is None else _buf(full, t.dtype, t.device, "rope " + name)
+           for name, t in (("Q", Q), ("K", K))]
+    agg.agg_rope_fwd(shape, rope, q_norm, k_norm, pos, Q, q_stride, K, k_stride, *out)
+    return out
+
+
+def residual_forward(residual, x, branch, want_h=True):
+    """h (None unless wanted) and n (None without a norm in front of the next branch)."""
+    h = _buf(tuple(x.shape), x.dtype, x.device, "residual h") if want_h else None
+    n = _buf(tuple(x.shape), x.dtype, x.device, "residual n") if residual.pre.kind else None
+    agg.agg_residual_norm_fwd(x.shape[0], x.shape[1], residual, x, branch, h, n)
+    return h, n
+
+
+def mx4_quantize(x, K=None, poison=True):
+    """(codes, scales) of bf16 [rows, K] (K given: the first K channels of longer rows)."""
+    rows, stride = x.shape
+    K = stride if K is None else K
+    codes = _buf((rows, agg.agg_mx4_code_stride(K)), torch.uint8, x.device, "codes")
+    scales = _buf((rows, agg.agg_mx4_scale_stride(K)), torch.uint8, x.device, "scales")
+    if poison:
+        codes.fill_(0x5A)
+        scales.fill_(0x5A)
+    agg.agg_mx4_quantize(rows, K, x, stride, codes, scales)
+    return codes, scales
+
+
+def mx4_dequantize(held, K):
+    codes, scales = held
+    x = _buf((codes.shape[0], K), torch.bfloat16, codes.device, "values")
+    agg.agg_mx4_dequantize(codes.shape[0], K, codes, scales, x)
+    return x
+
+
+def mx4_linear(a, weights, K, biases=None, residual=None, res_scale=None):
+    """The products of `a` (codes, scales) with up to three matrices held so."""
+    rows, N = a[0].shape[0], weights[0][0].shape[0]
+    out = [_buf((rows, N), torch.bfloat16, a[0].device, "product %d" % i) for i in range(len(weights))]
+    plan = agg.make_mx4_linear(weights, out, biases, residual, res_scale)
+    agg.agg_mx4_linear_fwd(rows, N, K, plan, *a)
+    return out
+
+
+def block_ex_forward(shape, mode, wts, options, x):
+    """agg_global_block_ex_fwd on buffers of its own: y and n (None without a norm behind)."""
+    cw = agg.make_block_weights(wts["ln_gamma"], wts["ln_beta"], wts["ln_eps"], wts["w_q"],
+                                wts["w_k"], wts["w_v"], wts["w_o"], wts.get("b_q"), wts.get("b_k"),
+                                wts.get("b_v"), wts.get("b_o"))
+    nws = agg.agg_block_ex_workspace_bytes(shape, mode, options)
+    ws = _buf(nws, torch.uint8, x.device, "block workspace")
+    ws.fill_(0xFF)
+    y = _buf(tuple(x.shape), x.dtype, x.device, "block y")
+    n = _buf(tuple(x.shape), x.dtype, x.device, "block n") if options.residual.pre.kind else None
+    agg.agg_global_block_ex_fwd(shape, mode, cw, options, x, y, n, ws, nws)
+    return y, n
