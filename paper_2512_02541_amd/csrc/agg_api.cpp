@@ -523,7 +523,9 @@ int make_mx4_args(int64_t rows, int32_t N, int32_t K, const agg_mx4_linear* l, c
   int rc = check_mx4(rows, K);
   if (rc != AGG_OK) return rc;
   if (N < 1 || N % 8 != 0 || l->count < 1 || l->count > 3) return AGG_ERR_SHAPE;
-  if (N > (1 << 21)) return AGG_ERR_OVERFLOW;
+  // a tile's rows of codes are addressed with 32 bits, tiles counted with 31
+  if (K > (1 << 22) || N > (1 << 21)) return AGG_ERR_OVERFLOW;
+  if (rows / 64 + 1 > (int64_t)INT32_MAX / ((N / 64 + 1) * (int64_t)l->count)) return AGG_ERR_OVERFLOW;
   if ((l->residual && l->count != 1) || (l->res_scale && !l->residual)) return AGG_ERR_SHAPE;
   if (rows > 0 && (!codes || !scales)) return AGG_ERR_NULL;
   if (misaligned(codes) || misaligned(scales) || misaligned(l->residual) || misaligned(l->res_scale))

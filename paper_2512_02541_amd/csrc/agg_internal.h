@@ -210,7 +210,9 @@ struct Mx4LinearArgs {
   int64_t rows;
   int32_t N, K, count;
   int32_t code_stride, scale_stride;
-  int32_t gn;  // channel tiles of a matrix (set by launch_mx4_linear)
+  int64_t gm;  // token tiles, and channel tiles of a matrix (set by launch_mx4_linear)
+  int32_t gn;
+  int32_t by_channels;  // the order of the tiles
 };
 hipError_t launch_mx4_linear(const Mx4LinearArgs& args, hipStream_t st);
 

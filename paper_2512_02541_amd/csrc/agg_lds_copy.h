@@ -30,6 +30,13 @@ __device__ __forceinline__ void dma16(const void* base, uint32_t voff, uint32_t 
                : "v"(voff), "s"(base), "s"(m0)
                : "memory");
 }
+// The same, four bytes a lane: lane i lands at m0 + 4 i.
+__device__ __forceinline__ void dma4(const void* base, uint32_t voff, uint32_t m0) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1"
+               :
+               : "v"(voff), "s"(base), "s"(m0)
+               : "memory");
+}
 // a pointer every lane agrees on, as two scalar registers (what the copy's base operand needs)
 __device__ __forceinline__ const uint16_t* uniform_ptr(const uint16_t* q) {
   const uint64_t v = (uint64_t)(uintptr_t)q;

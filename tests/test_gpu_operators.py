@@ -400,6 +400,44 @@ def test_product_sizes(rows, N, K, count):
     product_case(rows, N, K, count, True, count == 1)
 
 
+# (rows, N, K, matrices, residual): odd sizes that reach every kernel, and the sizes at which one hands over to the
+# next (test_operator_plan.py checks where they lead)
+FEW = [(1, 1024, 1024, 3, False), (32, 1024, 1024, 3, False), (63, 1000, 4096, 1, True), (127, 1024, 520, 1, True)]
+TILE64 = [(129, 1024, 1024, 1, True), (65, 1000, 4096, 1, False), (1023, 1032, 264, 3, False)]
+TILE128 = [(1374, 1024, 1024, 3, False), (5001, 1032, 264, 1, True), (4097, 1032, 1032, 1, False)]
+MANY = [(9001, 1032, 264, 1, True), (7601, 1032, 1040, 1, False), (10992, 520, 64, 3, False)]
+TILE256 = [(12001, 1032, 2056, 1, True), (12001, 1032, 1288, 2, False)]
+SPLIT = [(17001, 1032, 1040, 1, True), (16001, 1032, 1304, 2, False), (16700, 1024, 1288, 1, True)]
+PANEL = [(22001, 1000, 1000, 3, False), (22001, 1000, 696, 3, False), (22001, 1000, 264, 3, False),
+         (22001, 1000, 200, 3, False), (44000, 1032, 1024, 2, False), (2048 * 512 + 5, 64, 64, 1, False)]
+
+
+@pytest.mark.parametrize("rows, N, K, count, residual", FEW + TILE64 + TILE128 + MANY + TILE256 + SPLIT + PANEL)
+def test_product_kernels(rows, N, K, count, residual):
+    """Against float64 products on the GPU, the values themselves being exact."""
+    say("product kernel", rows, N, K, count, residual)
+    g = gen(rows + N + K)
+    x = (normal(g, rows, K) * torch.exp(normal(g, rows, 1))).to(torch.bfloat16)
+    a = harness.mx4_quantize(x)
+    av = harness.mx4_dequantize(a, K).double()
+    ws = [harness.mx4_quantize((normal(g, N, K) * K ** -0.5).to(torch.bfloat16)) for _ in range(count)]
+    bs = [normal(g, N) if i != 1 else None for i in range(count)]
+    res, rs = (normal(g, rows, N).to(torch.bfloat16), normal(g, N)) if residual else (None, None)
+    out = harness.mx4_linear(a, ws, K, bs, res, rs)
+    for i in range(count):
+        wv = harness.mx4_dequantize(ws[i], K).double().t().contiguous()
+        for at in range(0, rows, 1 << 15):
+            part = slice(at, min(rows, at + (1 << 15)))
+            want, size = av[part] @ wv, av[part].abs() @ wv.abs()
+            if bs[i] is not None:
+                want, size = want + bs[i].double(), size + bs[i].double().abs()
+            if residual:
+                want, size = want * rs.double() + res[part].double(), size * rs.double().abs() + res[part].double().abs()
+            tol = HALF * want.abs() + (2 * -(-K // 128) + 4) * 2.0 ** -24 * size
+            bad = ~((out[i][part].double() - want).abs() <= tol)
+            assert not bad.any(), (i, at, bad.nonzero()[:4].tolist())
+
+
 def test_product_in_place_on_the_residual():
     say("product in place")
     for rows in (5, 700):
