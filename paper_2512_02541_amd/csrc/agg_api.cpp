@@ -374,7 +374,7 @@ int make_norm(const agg_norm* n, SeamNorm* out) {
 // The pairs of channels that turn, their axes and frequencies (agg.h).
 int make_rope(const agg_rope* r, RopeArgs* a) {
   a->pairs = 0;
-  for (int c = 0; c < kHeadDim; ++c) a->channel[c] = (uint16_t)c;
+  for (int c = 0; c < kHeadDim; ++c) a->other[c] = (uint8_t)c;
   if (!r) return AGG_OK;
   if (r->pairing != AGG_ROPE_SECTIONS && r->pairing != AGG_ROPE_NEIGHBOURS && r->pairing != AGG_ROPE_HEAD)
     return AGG_ERR_SHAPE;
@@ -388,29 +388,27 @@ int make_rope(const agg_rope* r, RopeArgs* a) {
   if (!(r->base >= 1.0f) || !(r->base < INFINITY)) return AGG_ERR_SHAPE;
   a->t0 = r->t0;
   a->patch0 = r->patch0;
+  // frequencies in 2^-64 turns per position, each the one before times a constant: 64 bits of mantissa
+  // lose at most 2^-59 of a frequency over 32 steps (a power for each took the call 10 us)
+  const long double whole = 18446744073709551616.0L / (2 * 3.14159265358979323846264338327950288L);
+  long double freq = whole, ratio = 1;
+  if (r->pairing == AGG_ROPE_HEAD && turned) ratio = powl((long double)r->base, -2.0L / turned);
   int start = 0, p = 0;
   for (int axis = 0; axis < 3; ++axis) {
+    if (r->pairing != AGG_ROPE_HEAD && d[axis]) {
+      freq = whole;
+      ratio = powl((long double)r->base, -2.0L / d[axis]);
+    }
     for (int j = 0; j < d[axis] / 2; ++j, ++p) {
-      int lo, hi;
-      long double e;
-      if (r->pairing == AGG_ROPE_HEAD) {
-        lo = p;
-        hi = p + turned / 2;
-        e = 2.0L * p / turned;
-      } else if (r->pairing == AGG_ROPE_SECTIONS) {
-        lo = start + j;
-        hi = start + j + d[axis] / 2;
-        e = 2.0L * j / d[axis];
-      } else {
-        lo = start + 2 * j;
-        hi = lo + 1;
-        e = 2.0L * j / d[axis];
-      }
-      const long double pi = 3.14159265358979323846264338327950288L;
-      a->freq[p] = (uint64_t)(powl((long double)r->base, -e) / (2 * pi) * 18446744073709551616.0L);
+      const int lo = r->pairing == AGG_ROPE_HEAD ? p : start + (r->pairing == AGG_ROPE_SECTIONS ? j : 2 * j);
+      const int hi = lo + (r->pairing == AGG_ROPE_HEAD ? turned / 2 : r->pairing == AGG_ROPE_SECTIONS ? d[axis] / 2 : 1);
+      a->freq[p] = (uint64_t)freq;
+      freq *= ratio;
       a->axis[p] = (uint8_t)axis;
-      a->channel[lo] = (uint16_t)(hi | p << 6 | 0x1000);
-      a->channel[hi] = (uint16_t)(lo | p << 6 | 0x800 | 0x1000);
+      a->first[p] = (uint8_t)lo;
+      a->second[p] = (uint8_t)hi;
+      a->other[lo] = (uint8_t)(hi | 0x80);
+      a->other[hi] = (uint8_t)(lo | 0x80);
     }
     start += d[axis];
   }

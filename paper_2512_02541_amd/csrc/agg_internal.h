@@ -174,9 +174,8 @@ struct RopeArgs {
   int32_t tokens;         // of a wavefront's turn (set by launch_rope)
   uint64_t freq[kHeadDim / 2];     // of a pair, in 2^-64 turns per position
   uint8_t axis[kHeadDim / 2];      // 0 time, 1 row, 2 column
-  // of a channel: its pair's other channel (bits 0..5), the pair (6..10), whether the other's share
-  // is added (11), whether it turns at all (12)
-  uint16_t channel[kHeadDim];
+  uint8_t first[kHeadDim / 2], second[kHeadDim / 2];  // its channels
+  uint8_t other[kHeadDim];         // of a channel: its pair's other one, bit 7: it turns
 };
 hipError_t launch_rope(const RopeArgs& args, hipStream_t st);
 

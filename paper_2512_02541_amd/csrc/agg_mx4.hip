@@ -356,13 +356,16 @@ __global__ __launch_bounds__(64 * kWM * kWN, kPerSimd) void mx4_tile_kernel(Mx4L
   typedef uint32_t Run __attribute__((ext_vector_type(kNT / 2)));  // kNT channels of a token
   const int64_t corner = (m0 + wm + eg) * p.N + n;
   const int64_t left = p.rows - (m0 + wm + eg);
+  Run x[kMT][4];  // of the residual, requested at once
+  if (p.residual)
 #pragma unroll
-  for (int t = 0; t < kMT; ++t) {
-    Run x[4];
-    if (p.residual)
+    for (int t = 0; t < kMT; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        if (16 * t + r < left) x[r] = *reinterpret_cast<const Run*>(p.residual + corner + (int64_t)(16 * t + r) * p.N);
+        if (16 * t + r < left)
+          x[t][r] = *reinterpret_cast<const Run*>(p.residual + corner + (int64_t)(16 * t + r) * p.N);
+#pragma unroll
+  for (int t = 0; t < kMT; ++t)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       if (16 * t + r >= left) continue;
@@ -372,7 +375,7 @@ __global__ __launch_bounds__(64 * kWM * kWN, kPerSimd) void mx4_tile_kernel(Mx4L
       if (p.residual)
 #pragma unroll
         for (int u = 0; u < kNT; ++u) {
-          const uint32_t w = x[r][u / 2];
+          const uint32_t w = x[t][r][u / 2];
           y[u] = (u % 2 ? __uint_as_float(w & 0xFFFF0000u) : bf16_of(w)) + scale[u] * y[u];
         }
       Run out;
@@ -380,7 +383,6 @@ __global__ __launch_bounds__(64 * kWM * kWN, kPerSimd) void mx4_tile_kernel(Mx4L
       for (int u = 0; u < kNT / 2; ++u) out[u] = pack2(y[2 * u], y[2 * u + 1]);
       __builtin_nontemporal_store(out, reinterpret_cast<Run*>(p.y[which] + corner + (int64_t)(16 * t + r) * p.N));
     }
-  }
 }
 
 template <int kTM, int kTN, int kWM, int kWN, int kStages, int kPerSimd>

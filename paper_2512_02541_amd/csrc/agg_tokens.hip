@@ -2,6 +2,7 @@
 // seam between one branch and the next (norm, gate, residual scale, sum, norm).  Both are single passes
 // whose bound is HBM: every row is read once, held in registers in float32 and written once.
 #include "agg_internal.h"
+#include "agg_lds_copy.h"
 
 namespace agg {
 
@@ -41,6 +42,22 @@ __device__ inline void load8(const float* p, int at, float other, float (&v)[8])
   }
 }
 
+// the sum over eight neighbouring lanes, in all of them: two exchanges within four lanes, one between them
+__device__ inline float sum_of_8(float v) {
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xB1, 0xF, 0xF, true));   // lane ^ 1
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4E, 0xF, 0xF, true));   // lane ^ 2
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xF, 0xF, true));  // 7 - lane
+  return v;
+}
+
+// ... over the wavefront
+__device__ inline float sum_of_wave(float v) {
+  v = sum_of_8(v);
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xF, 0xF, true));  // 15 - lane
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
+}
+
 // orders a wavefront's LDS writes before its own later reads
 __device__ inline void wave_lds_fence() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
@@ -66,24 +83,23 @@ constexpr int kHeadStride = kHeadDim + 4;    // floats of a head in LDS: 16-byte
 
 __global__ __launch_bounds__(kRopeThreads, 4) void rope_kernel(RopeArgs a) {
   __shared__ __align__(16) float heads[kRopeWaves][8][kHeadStride];
-  __shared__ __align__(16) f32x2 turns[kRopeWaves][kRopeMaxTokens][kRopePairs];
+  __shared__ __align__(16) f32x2 turns[kRopeWaves][kRopeMaxTokens][kHeadDim];  // of a channel: cosine, signed sine
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int group = lane >> 3, c0 = (lane & 7) * 8;  // this lane's head among eight, its first channel
   const int H = a.H;
 
-  // each channel's other one, its pair and the sign of the other's share; unturned: itself, none
-  int other[8], pair[8];
-  float sign[8];
+  // each channel's other one, and whether it turns at all
+  int other[8];
   uint32_t turned = 0;
+  const bool all_turn = a.pairs == kRopePairs;
   if (a.pairs) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const uint32_t m = a.channel[c0 + i];
-      other[i] = m & 63;
-      pair[i] = (m >> 6) & 31;
-      sign[i] = (m & 0x800) ? 1.f : -1.f;
-      if (m & 0x1000) turned |= 1u << i;
+      other[i] = a.other[c0 + i] & 63;
+      if (a.other[c0 + i] & 0x80) turned |= 1u << i;
     }
+    // channels that no pair writes
+    for (int i = 0; i < a.tokens; ++i) turns[wave][i][lane] = f32x2{1.f, 0.f};
   }
   float g[2][8], b[2][8];
 #pragma unroll
@@ -94,20 +110,33 @@ __global__ __launch_bounds__(kRopeThreads, 4) void rope_kernel(RopeArgs a) {
   float* const head = heads[wave][group];
 
   const int64_t step = (int64_t)gridDim.x * kRopeWaves * a.tokens;
+  const int h0 = group % H, sub0 = group / H;
   for (int64_t t0 = ((int64_t)blockIdx.x * kRopeWaves + wave) * a.tokens; t0 < a.total; t0 += step) {
     const int here = (int)min((int64_t)a.tokens, a.total - t0);
+    // a turn's heads, eight at a time; a round's rows are requested while the one before is worked on
+    int h = h0, sub = sub0;
+    u32x4 ahead[2];
+    auto request = [&]() {
+      if (sub < here)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          if (a.in[t])
+            ahead[t] = *reinterpret_cast<const u32x4*>(a.in[t] + (t0 + sub) * a.stride[t] + h * kHeadDim + c0);
+    };
+    request();
     if (a.pairs) {
       wave_lds_fence();  // the last turn's reads are done
       for (int i = lane; i < here * kRopePairs; i += 64) {
-        const int p = i % kRopePairs, sub = i / kRopePairs;
+        const int p = i % kRopePairs, of = i / kRopePairs;
         if (p < a.pairs) {
-          const int64_t tok = t0 + sub;
+          const int64_t tok = t0 + of;
           const int axis = a.axis[p];
           int32_t pos;
           if (a.pos) {
             pos = a.pos[tok * 3 + axis];
           } else {
-            const uint32_t in_seq = (uint32_t)(tok % a.NQ);  // < 2^31
+            // < 2^31; a 64-bit division only where the token's number needs it
+            const uint32_t in_seq = a.total >> 32 ? (uint32_t)(tok % a.NQ) : (uint32_t)tok % (uint32_t)a.NQ;
             const uint32_t frame = in_seq / (uint32_t)a.L;
             const int32_t patch = (int32_t)(in_seq % (uint32_t)a.L) - a.P;
             if (axis == 0) pos = a.t0 + (int32_t)frame;
@@ -118,19 +147,21 @@ __global__ __launch_bounds__(kRopeThreads, 4) void rope_kernel(RopeArgs a) {
           // the signed high half: a turn is 2^32, half a turn 2^31
           float s, c;
           sincospif((float)(int32_t)(phase >> 32) * 0x1p-31f, &s, &c);
-          turns[wave][sub][p] = f32x2{c, s};
+          turns[wave][of][a.first[p]] = f32x2{c, -s};
+          turns[wave][of][a.second[p]] = f32x2{c, s};
         }
       }
       wave_lds_fence();
     }
-    for (int item = group; item < here * H; item += 8) {
-      const int sub = item / H, h = item - sub * H;
-      const int64_t tok = t0 + sub;
-      u32x4 raw[2];
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-        if (a.in[t])
-          raw[t] = *reinterpret_cast<const u32x4*>(a.in[t] + tok * a.stride[t] + h * kHeadDim + c0);
+    while (sub < here) {
+      u32x4 raw[2] = {ahead[0], ahead[1]};
+      const int at_h = h, at_sub = sub;
+      h += 8;
+      while (h >= H) {
+        h -= H;
+        ++sub;
+      }
+      request();
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         if (!a.in[t]) continue;
@@ -142,9 +173,7 @@ __global__ __launch_bounds__(kRopeThreads, 4) void rope_kernel(RopeArgs a) {
           if (kind == AGG_NORM_LAYER) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) mean += x[i];
-#pragma unroll
-            for (int o = 1; o < 8; o <<= 1) mean += __shfl_xor(mean, o);
-            mean *= 1.f / kHeadDim;
+            mean = sum_of_8(mean) * (1.f / kHeadDim);
           }
           float sq = 0.f;
 #pragma unroll
@@ -152,9 +181,7 @@ __global__ __launch_bounds__(kRopeThreads, 4) void rope_kernel(RopeArgs a) {
             x[i] -= mean;
             sq += x[i] * x[i];
           }
-#pragma unroll
-          for (int o = 1; o < 8; o <<= 1) sq += __shfl_xor(sq, o);
-          const float r = rsqrtf(sq * (1.f / kHeadDim) + a.norm[t].eps);
+          const float r = rsqrtf(sum_of_8(sq) * (1.f / kHeadDim) + a.norm[t].eps);
 #pragma unroll
           for (int i = 0; i < 8; ++i) x[i] = x[i] * r * g[t][i] + b[t][i];
         }
@@ -163,14 +190,24 @@ __global__ __launch_bounds__(kRopeThreads, 4) void rope_kernel(RopeArgs a) {
           *reinterpret_cast<f32x4*>(head + c0) = f32x4{x[0], x[1], x[2], x[3]};
           *reinterpret_cast<f32x4*>(head + c0 + 4) = f32x4{x[4], x[5], x[6], x[7]};
           wave_lds_fence();
+          float y[8];
+          f32x4 cs[4];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const f32x2 cs = turns[wave][sub][pair[i]];
-            const float y = x[i] * cs[0] + sign[i] * head[other[i]] * cs[1];
-            x[i] = (turned >> i) & 1 ? y : x[i];
+          for (int i = 0; i < 4; ++i) cs[i] = *reinterpret_cast<const f32x4*>(&turns[wave][at_sub][c0 + 2 * i]);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) y[i] = head[other[i]];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) y[i] = x[i] * cs[i / 2][i % 2 * 2] + y[i] * cs[i / 2][i % 2 * 2 + 1];
+          if (all_turn) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = y[i];
+          } else {  // by selection: an infinity times 0 is none of the other channels' business
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = (turned >> i) & 1 ? y[i] : x[i];
           }
         }
-        *reinterpret_cast<u32x4*>(a.out[t] + (tok * H + h) * kHeadDim + c0) = pack8(x);
+        __builtin_nontemporal_store(
+            pack8(x), reinterpret_cast<u32x4*>(a.out[t] + ((t0 + at_sub) * H + at_h) * kHeadDim + c0));
       }
     }
   }
@@ -178,7 +215,8 @@ __global__ __launch_bounds__(kRopeThreads, 4) void rope_kernel(RopeArgs a) {
 
 hipError_t launch_rope(const RopeArgs& args, hipStream_t st) {
   RopeArgs a = args;
-  a.tokens = a.H >= 4 ? 2 : kRopeMaxTokens / a.H;
+  // two tokens a turn fill the lanes that work out the angles; few tokens are spread over more wavefronts
+  a.tokens = a.H < 4 ? kRopeMaxTokens / a.H : a.total <= 4096 ? 1 : 2;
   const int64_t turns = (a.total + a.tokens - 1) / a.tokens;
   const int64_t groups = (turns + kRopeWaves - 1) / kRopeWaves;
   (void)hipGetLastError();
@@ -187,122 +225,313 @@ hipError_t launch_rope(const RopeArgs& args, hipStream_t st) {
 }
 
 // ---------------------------------------------------------------------------
-// h = x + gate * scale * post(branch),  n = pre(h): one wavefront per row, the row in registers in
-// float32, statistics as in layernorm_kernel (mean, then variance of the centred values).
-// kChunks = 16-byte chunks per lane.
+// h = x + gate * scale * post(branch),  n = pre(h).  A row is in registers in float32, statistics as in
+// layernorm_kernel (mean, then variance of the centred values); norms' parameters stay in registers
+// from row to row, and the next row is requested before the present one is worked on.
+// Rows of up to 1024 channels: one wavefront each, kPer 16-byte chunks a lane.  Longer ones: the
+// whole workgroup, of as many wavefronts as the row fills, whose sums meet in LDS.
 // ---------------------------------------------------------------------------
-constexpr int kSeamThreads = 256;
-
 namespace {
 
-template <int kChunks>
-__device__ inline void norm_row(float (&v)[kChunks][8], const SeamNorm& n, int lane, int nchunk, float inv_c) {
-  float mean = 0.f;
-  if (n.kind == AGG_NORM_LAYER) {
+// what a norm multiplies by and adds, of this thread's channels
+template <int kPer>
+struct SeamParams {
+  float gamma[kPer][8], beta[kPer][8];
+};
+
+template <int kPer, bool kAcross>
+struct SeamRow {
+  float v[kPer][8];
+  // the sum over the row; kAcross: over the workgroup's wavefronts too (`turn` alternates the slots, so that one
+  // barrier a sum is enough: a slot is written again only behind the next sum's barrier)
+  __device__ static inline float total(float x, float (*slots)[8], int& turn, int waves) {
+    x = sum_of_wave(x);
+    if constexpr (kAcross) {
+      if ((threadIdx.x & 63) == 0) slots[turn][threadIdx.x >> 6] = x;
+      lds_barrier();  // (of LDS alone: the next row's loads stay under way)
+      float all = 0.f;
+      for (int w = 0; w < waves; ++w) all += slots[turn][w];
+      x = all;
+      turn ^= 1;
+    }
+    return x;
+  }
+  __device__ inline void norm(const SeamNorm& n, const SeamParams<kPer>& p, const bool (&has)[kPer], float inv_c,
+                              float (*slots)[8], int& turn, int waves) {
+    float mean = 0.f;
+    if (n.kind == AGG_NORM_LAYER) {
 #pragma unroll
-    for (int c = 0; c < kChunks; ++c)
-      if (lane + 64 * c < nchunk)
+      for (int c = 0; c < kPer; ++c)
 #pragma unroll
         for (int i = 0; i < 8; ++i) mean += v[c][i];
+      mean = total(mean, slots, turn, waves) * inv_c;
+    }
+    float sq = 0.f;
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) mean += __shfl_xor(mean, o);
-    mean *= inv_c;
-  }
-  float sq = 0.f;
-#pragma unroll
-  for (int c = 0; c < kChunks; ++c)
-    if (lane + 64 * c < nchunk)
+    for (int c = 0; c < kPer; ++c)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        v[c][i] -= mean;
+        v[c][i] = has[c] ? v[c][i] - mean : 0.f;
         sq += v[c][i] * v[c][i];
       }
+    const float r = rsqrtf(total(sq, slots, turn, waves) * inv_c + n.eps);
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) sq += __shfl_xor(sq, o);
-  const float r = rsqrtf(sq * inv_c + n.eps);
+    for (int c = 0; c < kPer; ++c)
 #pragma unroll
-  for (int c = 0; c < kChunks; ++c) {
-    const int ch = lane + 64 * c;
-    if (ch < nchunk) {
-      float g[8], b[8];
-      load8(n.gamma, ch * 8, 1.f, g);
-      load8(n.beta, ch * 8, 0.f, b);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[c][i] = v[c][i] * r * g[i] + b[i];
-    }
+      for (int i = 0; i < 8; ++i) v[c][i] = v[c][i] * r * p.gamma[c][i] + p.beta[c][i];
   }
-}
+};
 
 }  // namespace
 
-template <int kChunks>
-__global__ __launch_bounds__(kSeamThreads) void seam_kernel(SeamArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * (kSeamThreads / 64) + (threadIdx.x >> 6);
-  if (row >= a.rows) return;
+template <int kPer, bool kAcross>
+__global__ __launch_bounds__(kAcross ? 512 : 256) void seam_kernel(SeamArgs a) {
+  __shared__ float slots[2][8];
+  const int waves = blockDim.x >> 6;
+  const int at = kAcross ? threadIdx.x : threadIdx.x & 63;  // this thread among those of a row
   const int nchunk = a.C / 8;
   const float inv_c = 1.f / (float)a.C;
-  float v[kChunks][8];
-  u32x4 xr[kChunks];
+  bool has[kPer];
+  int off[kPer];  // of this thread's chunks; the missing ones read the row's first
 #pragma unroll
-  for (int c = 0; c < kChunks; ++c) {
-    const int ch = lane + 64 * c;
-    if (ch < nchunk) {
-      xr[c] = *reinterpret_cast<const u32x4*>(a.x + row * a.C + ch * 8);
-      if (a.branch) unpack8(*reinterpret_cast<const u32x4*>(a.branch + row * a.C + ch * 8), v[c]);
-    }
+  for (int c = 0; c < kPer; ++c) {
+    const int ch = at + c * (kAcross ? (int)blockDim.x : 64);
+    has[c] = ch < nchunk;
+    off[c] = has[c] ? ch * 8 : 0;
   }
-  if (a.branch) {
-    if (a.post.kind != AGG_NORM_NONE) norm_row<kChunks>(v, a.post, lane, nchunk, inv_c);
-    const uint16_t* gate = a.gate ? a.gate + row / a.gate_rows * a.C : nullptr;
+  SeamParams<kPer> post, pre;
+  float scale[kPer][8];
 #pragma unroll
-    for (int c = 0; c < kChunks; ++c) {
-      const int ch = lane + 64 * c;
-      if (ch < nchunk) {
-        float s[8], x[8];
-        load8(a.scale, ch * 8, 1.f, s);
+  for (int c = 0; c < kPer; ++c) {
+    load8(a.post.gamma, off[c], 1.f, post.gamma[c]);
+    load8(a.post.beta, off[c], 0.f, post.beta[c]);
+    load8(a.pre.gamma, off[c], 1.f, pre.gamma[c]);
+    load8(a.pre.beta, off[c], 0.f, pre.beta[c]);
+    load8(a.scale, off[c], 1.f, scale[c]);
+  }
+  const int64_t first = kAcross ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t step = kAcross ? (int64_t)gridDim.x : (int64_t)gridDim.x * 4;
+  u32x4 xr[kPer], br[kPer], gr[kPer];
+  auto request = [&](int64_t row) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[c][i] *= s[i];
-        if (gate) {
-          unpack8(*reinterpret_cast<const u32x4*>(gate + ch * 8), s);
+    for (int c = 0; c < kPer; ++c) {
+      xr[c] = *reinterpret_cast<const u32x4*>(a.x + row * a.C + off[c]);
+      if (a.branch) br[c] = *reinterpret_cast<const u32x4*>(a.branch + row * a.C + off[c]);
+      if (a.gate)  // rows < 2^31 and gate_rows <= 2^31
+        gr[c] = *reinterpret_cast<const u32x4*>(a.gate + (int64_t)((uint32_t)row / (uint32_t)a.gate_rows) * a.C + off[c]);
+    }
+  };
+  int turn = 0;
+  if (first < a.rows) request(first);
+  for (int64_t row = first; row < a.rows; row += step) {
+    SeamRow<kPer, kAcross> r;
+    float x[kPer][8], g[kPer][8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) v[c][i] *= s[i];
-        }
-        unpack8(xr[c], x);
+    for (int c = 0; c < kPer; ++c) {
+      unpack8(xr[c], x[c]);
+      if (a.branch) unpack8(br[c], r.v[c]);
+      if (a.gate) unpack8(gr[c], g[c]);
+    }
+    if (row + step < a.rows) request(row + step);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[c][i] += x[i];
+    for (int c = 0; c < kPer; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[c][i] = has[c] ? x[c][i] : 0.f;
+        r.v[c][i] = has[c] && a.branch ? r.v[c][i] : 0.f;
       }
+    if (a.branch) {
+      if (a.post.kind != AGG_NORM_NONE) r.norm(a.post, post, has, inv_c, slots, turn, waves);
+#pragma unroll
+      for (int c = 0; c < kPer; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          r.v[c][i] *= scale[c][i];
+          if (a.gate) r.v[c][i] *= g[c][i];
+          r.v[c][i] += x[c][i];
+        }
+#pragma unroll
+      for (int c = 0; c < kPer; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r.v[c][i] = has[c] ? r.v[c][i] : 0.f;
+    } else {
+#pragma unroll
+      for (int c = 0; c < kPer; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r.v[c][i] = x[c][i];
     }
-  } else {
+    if (a.h) {
 #pragma unroll
-    for (int c = 0; c < kChunks; ++c)
-      if (lane + 64 * c < nchunk) unpack8(xr[c], v[c]);
-  }
-  if (a.h) {
+      for (int c = 0; c < kPer; ++c)
+        if (has[c]) *reinterpret_cast<u32x4*>(a.h + row * a.C + off[c]) = pack8(r.v[c]);
+    }
+    if (a.pre.kind != AGG_NORM_NONE) {
+      r.norm(a.pre, pre, has, inv_c, slots, turn, waves);
 #pragma unroll
-    for (int c = 0; c < kChunks; ++c)
-      if (lane + 64 * c < nchunk)
-        *reinterpret_cast<u32x4*>(a.h + row * a.C + (lane + 64 * c) * 8) = pack8(v[c]);
-  }
-  if (a.pre.kind != AGG_NORM_NONE) {
-    norm_row<kChunks>(v, a.pre, lane, nchunk, inv_c);
-#pragma unroll
-    for (int c = 0; c < kChunks; ++c)
-      if (lane + 64 * c < nchunk)
-        *reinterpret_cast<u32x4*>(a.n + row * a.C + (lane + 64 * c) * 8) = pack8(v[c]);
+      for (int c = 0; c < kPer; ++c)
+        if (has[c]) *reinterpret_cast<u32x4*>(a.n + row * a.C + off[c]) = pack8(r.v[c]);
+    }
   }
 }
 
-hipError_t launch_seam(const SeamArgs& a, hipStream_t st) {
-  const int64_t groups = (a.rows + kSeamThreads / 64 - 1) / (kSeamThreads / 64);
-  if (groups > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
-  const dim3 grid((unsigned)groups), block(kSeamThreads);
-  (void)hipGetLastError();
-  if (a.C <= 512 * 2) hipLaunchKernelGGL(seam_kernel<2>, grid, block, 0, st, a);
-  else if (a.C <= 512 * 4) hipLaunchKernelGGL(seam_kernel<4>, grid, block, 0, st, a);
-  else if (a.C <= 512 * 8) hipLaunchKernelGGL(seam_kernel<8>, grid, block, 0, st, a);
-  else hipLaunchKernelGGL(seam_kernel<16>, grid, block, 0, st, a);
+// ---------------------------------------------------------------------------
+// The same for many long rows: one wavefront a row again, kChunks chunks a lane, the parameters of all
+// channels in LDS (registers would hold too few wavefronts, and a row shared by a workgroup's
+// wavefronts fills the SIMDs unevenly unless they are a multiple of four).
+// ---------------------------------------------------------------------------
+constexpr int kLongThreads = 256;
+
+template <int kChunks>
+__global__ __launch_bounds__(kLongThreads, kChunks <= 4 ? 4 : kChunks <= 6 ? 3 : 2) void seam_long_kernel(SeamArgs a) {
+  extern __shared__ __align__(16) float params[];
+  const int lane = threadIdx.x & 63;
+  // kChunks is the row's number of 64-chunk runs: only the last one may be partial
+  const int nchunk = a.C / 8;
+  const bool in_last = lane + 64 * (kChunks - 1) < nchunk;
+  const int last_at = (in_last ? lane + 64 * (kChunks - 1) : 0) * 8;
+  auto at = [&](int c) { return c + 1 < kChunks ? lane * 8 + 512 * c : last_at; };
+  auto has = [&](int c) { return c + 1 < kChunks || in_last; };
+  const float inv_c = 1.f / (float)a.C;
+  const float* const from[5] = {a.post.gamma, a.post.beta, a.scale, a.pre.gamma, a.pre.beta};
+  int place[5], held = 0;  // of each parameter that is there
+#pragma unroll
+  for (int k = 0; k < 5; ++k) {
+    place[k] = -1;
+    if (!from[k]) continue;
+    place[k] = held * a.C;
+    ++held;
+    for (int c = threadIdx.x; c < a.C / 4; c += kLongThreads)
+      *reinterpret_cast<f32x4*>(params + place[k] + 4 * c) = *reinterpret_cast<const f32x4*>(from[k] + 4 * c);
+  }
+  __syncthreads();
+
+  auto norm = [&](float (&v)[kChunks][8], const SeamNorm& n, int gamma, int beta) {
+    float mean = 0.f;
+    if (n.kind == AGG_NORM_LAYER) {
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) mean += v[c][i];
+      mean = sum_of_wave(mean) * inv_c;
+    }
+    float sq = 0.f;
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        v[c][i] = has(c) ? v[c][i] - mean : 0.f;
+        sq += v[c][i] * v[c][i];
+      }
+    const float r = rsqrtf(sum_of_wave(sq) * inv_c + n.eps);
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[c][i] *= r;
+      if (gamma >= 0) {
+        float g[8];
+        load8(params + gamma, at(c), 1.f, g);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[c][i] *= g[i];
+      }
+      if (beta >= 0) {
+        float b[8];
+        load8(params + beta, at(c), 0.f, b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[c][i] += b[i];
+      }
+    }
+  };
+  const int64_t step = (int64_t)gridDim.x * (kLongThreads / 64);
+  for (int64_t row = (int64_t)blockIdx.x * (kLongThreads / 64) + (threadIdx.x >> 6); row < a.rows; row += step) {
+    u32x4 xr[kChunks], gr[kChunks];
+    float v[kChunks][8];
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) {
+      xr[c] = *reinterpret_cast<const u32x4*>(a.x + row * a.C + at(c));
+      u32x4 br = {0u, 0u, 0u, 0u};
+      if (a.branch) br = *reinterpret_cast<const u32x4*>(a.branch + row * a.C + at(c));
+      if (a.gate)  // rows < 2^31 and gate_rows <= 2^31
+        gr[c] = *reinterpret_cast<const u32x4*>(a.gate + (int64_t)((uint32_t)row / (uint32_t)a.gate_rows) * a.C + at(c));
+      unpack8(br, v[c]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[c][i] = has(c) ? v[c][i] : 0.f;
+    }
+    if (a.branch && a.post.kind != AGG_NORM_NONE) norm(v, a.post, place[0], place[1]);
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) {
+      float f[8];
+      if (place[2] >= 0) {
+        load8(params + place[2], at(c), 1.f, f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[c][i] *= f[i];
+      }
+      if (a.gate) {
+        unpack8(gr[c], f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[c][i] *= f[i];
+      }
+      unpack8(xr[c], f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[c][i] = has(c) ? v[c][i] + f[i] : 0.f;
+      if (a.h && has(c)) *reinterpret_cast<u32x4*>(a.h + row * a.C + at(c)) = pack8(v[c]);
+    }
+    if (a.pre.kind != AGG_NORM_NONE) {
+      norm(v, a.pre, place[3], place[4]);
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c)
+        if (has(c)) *reinterpret_cast<u32x4*>(a.n + row * a.C + at(c)) = pack8(v[c]);
+    }
+  }
+}
+
+template <int kPer, bool kAcross>
+static hipError_t launch_seam_rows(const SeamArgs& a, int threads, hipStream_t st) {
+  const int64_t groups = kAcross ? a.rows : (a.rows + 3) / 4;
+  const int64_t most = 256 * 2048 / threads;  // as many threads as the CUs hold
+  hipLaunchKernelGGL((seam_kernel<kPer, kAcross>), dim3((unsigned)(groups < most ? groups : most)), dim3(threads), 0, st, a);
   return hipGetLastError();
+}
+
+template <int kChunks>
+static hipError_t launch_seam_long(const SeamArgs& a, hipStream_t st) {
+  const float* const from[5] = {a.post.gamma, a.post.beta, a.scale, a.pre.gamma, a.pre.beta};
+  int held = 0;
+  for (const float* f : from) held += f != nullptr;
+  const int bytes = held * a.C * (int)sizeof(float);  // at most 80 KiB
+  const int64_t groups = (a.rows + kLongThreads / 64 - 1) / (kLongThreads / 64);
+  const int fit = bytes ? 160 * 1024 / bytes : 8;
+  const int64_t most = 256 * (kChunks <= 4 ? min(fit, 4) : kChunks <= 6 ? min(fit, 3) : 2);
+  if (bytes > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute((const void*)seam_long_kernel<kChunks>,
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, 80 * 1024);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(seam_long_kernel<kChunks>, dim3((unsigned)(groups < most ? groups : most)), dim3(kLongThreads),
+                     bytes, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_seam(const SeamArgs& args, hipStream_t st) {
+  SeamArgs a = args;
+  if (a.gate_rows > a.rows) a.gate_rows = a.rows;
+  if (a.post.kind == AGG_NORM_NONE) a.post.gamma = a.post.beta = nullptr;
+  if (a.pre.kind == AGG_NORM_NONE) a.pre.gamma = a.pre.beta = nullptr;
+  const int waves = (a.C / 8 + 63) / 64;  // one chunk a thread
+  (void)hipGetLastError();
+  if (waves == 1) return launch_seam_rows<1, false>(a, 256, st);
+  if (waves == 2) return launch_seam_rows<2, false>(a, 256, st);
+  if (waves > 8) return launch_seam_rows<2, true>(a, 512, st);
+  // Few rows: the whole workgroup on one of them. us for 1, 512, 1000 rows of 2112 channels with every part:
+  // 3.8, 5.1, 10.0 against 5.7, 7.0, 8.0 a wavefront each; 1, 768 rows of 4096: 3.7, 7.9 against 7.5, 10.4
+  if (a.rows <= 896) return launch_seam_rows<1, true>(a, 64 * waves, st);
+  switch (waves) {
+    case 3: return launch_seam_long<3>(a, st);
+    case 4: return launch_seam_long<4>(a, st);
+    case 5: return launch_seam_long<5>(a, st);
+    case 6: return launch_seam_long<6>(a, st);
+    case 7: return launch_seam_long<7>(a, st);
+  }
+  return launch_seam_long<8>(a, st);
 }
 
 }  // namespace agg
