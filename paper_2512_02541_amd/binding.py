@@ -57,7 +57,7 @@ def make_shape(B, N, n_h, n_w, n_special, H, D, s_h, s_w, keep_first_frame=1,
 
 
 _lib = None
-_raw_stream = None
+_raw_stream = _initialized = _device = None
 
 EXPORTS = [
     "agg_status_string", "agg_sigma_to_strides", "agg_kv_count", "agg_kv_indices_host",
@@ -263,9 +263,12 @@ def lib():
     L.agg_block_ex_workspace_bytes.argtypes = [shp, ctypes.c_int, opts]
     L.agg_global_block_ex_fwd.argtypes = [shp, ctypes.c_int, ctypes.POINTER(agg_block_weights), opts, vp, vp, vp,
                                           vp, ctypes.c_size_t, vp]
-    global _raw_stream
+    global _raw_stream, _initialized, _device
     # the current stream's handle without building a Stream object for it (3 us a call)
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    _initialized = torch.cuda.is_initialized
+    # (what torch.cuda.current_device asks once CUDA is initialised, which _stream sees to)
+    _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
     _lib = L
     return L
 
@@ -281,19 +284,18 @@ def _ptr(t):
     call itself)."""
     if t is None or isinstance(t, int):
         return t
-    if hasattr(t, "data_ptr"):
-        return t.data_ptr()
-    return t.ctypes.data
+    address = getattr(t, "data_ptr", None)
+    return t.ctypes.data if address is None else address()
 
 
 def _stream(stream):
     """Handle of `stream`, by default of the current device's current stream."""
     if stream is not None:
         return int(stream)
+    if _raw_stream is not None and _initialized():
+        return _raw_stream(_device())
     import torch
 
-    if _raw_stream is not None and torch.cuda.is_initialized():
-        return _raw_stream(torch.cuda.current_device())
     return torch.cuda.current_stream().cuda_stream
 
 
