@@ -237,6 +237,24 @@ def test_residual_widths(C):
     seam_case(3, C, "none", "rms", False, 0, affine=False)
 
 
+@pytest.mark.parametrize("C", [1032, 1536, 1544, 2048, 2056, 2112, 2560, 2568, 3064, 3584, 3592, 4088, 4096, 4104])
+def test_residual_long_rows(C):
+    """More rows than few, a wavefront each with the parameters in LDS: every width of 512 channels, its ends,
+    and the most parameters that there can be."""
+    say("residual long rows", C)
+    seam_case(1003, C, "layer", "layer", True, 261)
+    seam_case(897, C, "none", "rms", False, 0, affine=False)
+    seam_case(2501, C, "rms", "none", True)
+
+
+@pytest.mark.parametrize("rows", [896, 897])
+def test_residual_parts_of_long_rows(rows):
+    say("residual parts of long rows", rows)
+    for post, pre, branch, want_h in (("none", "layer", False, True), ("none", "rms", False, False),
+                                      ("layer", "none", True, True), ("none", "none", True, True)):
+        seam_case(rows, 1032, post, pre, branch, 5 if branch else 0, branch, want_h)
+
+
 @pytest.mark.parametrize("rows", [1, 2, 3, 4, 5, 261, 4099, 20011])
 def test_residual_rows(rows):
     say("residual rows", rows)

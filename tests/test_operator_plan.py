@@ -1,6 +1,8 @@
 """Which kernel a product of 4-bit floats runs, without a GPU: the plan is plain host code, compiled
 here by itself.  The GPU tests name sizes for every kernel and border; this file checks that they
 still lead there."""
+import os
+import re
 import subprocess
 
 import pytest
@@ -58,3 +60,57 @@ def test_plans_are_sound(plan):
         assert kernel != "panel" or (K <= 1024 and not residual)
         if kernel == "few":
             assert -(-rows // 16) * -(-N // 16) * count <= 512
+
+
+@pytest.fixture(scope="module")
+def assembly(tmp_path_factory):
+    out = tmp_path_factory.mktemp("asm") / "agg_mx4.s"
+    subprocess.check_call([b.HIPCC, *b.FLAGS, "-I", os.path.join(b.ROOT, "include"), "-I", b.CSRC, "-S",
+                           "--cuda-device-only", os.path.join(b.CSRC, "agg_mx4.hip"), "-o", str(out)],
+                          stderr=subprocess.DEVNULL)
+    return out.read_text()
+
+
+def test_product_kernels_leave_m0_to_their_copy_statements(assembly):
+    """The copies global -> LDS set M0 inside assembly statements without declaring it: sound only
+    while no instruction that the compiler emits touches M0."""
+    inside, copies, offenders = False, 0, []
+    for line in assembly.splitlines():
+        code = line.split(";")[0] if not line.lstrip().startswith(";;#") else line
+        if "#ASMSTART" in line:
+            inside = True
+        elif "#ASMEND" in line:
+            inside = False
+        elif inside:
+            copies += "global_load_lds_dword" in code
+        elif re.search(r"\bm0\b", code):
+            offenders.append(line.strip())
+    assert copies >= 32, "the copy statements were not found"
+    assert not offenders, offenders[:5]
+
+
+def test_panels_store_as_often_as_their_waits_count(assembly):
+    """A pass's copies are awaited by the number of younger accesses, three passes' stores among them.
+    Were the compiler to merge stores, or to put anything into scratch memory between them, that wait
+    would end early: a whole pass's stores are exactly 16 in one run without a branch, for the
+    wavefronts that store at a pass's end and those that store at the next one's beginning, and in the loop every
+    wait that is not one of the three written ones belongs to the loading of a panel."""
+    kernels = re.findall(r"^(\S*mx4_panel_kernelILi(\d)E\S*):[^\n]*\n(.*?)^\.Lfunc_end", assembly, flags=re.M | re.S)
+    assert len(kernels) == 2, [k[0] for k in kernels]
+    for name, steps, body in kernels:
+        assert "scratch_" not in body, name
+        loop = body[:body.rindex("v_mfma")]
+        runs, run = [], 0
+        for line in body.splitlines():
+            if re.match(r"\s+\w*store", line):
+                assert "global_store_dwordx2" in line, (name, line)
+                run += 1
+            elif re.match(r"\s+s_c?branch", line) or re.match(r"\.LBB", line):
+                runs.append(run)
+                run = 0
+        assert runs.count(16) >= 2 and set(runs) <= {0, 1, 15, 16}, (name, runs)
+        group = int(steps) // 2 + 2
+        waits = [int(w) for w in re.findall(r"s_waitcnt vmcnt\((\d+)\)\n", loop)]
+        assert 2 * group + 3 * 16 in waits and 2 * group in waits, (name, waits)
+        copies = re.findall(r"global_load_lds_dword(?:x4)?", body)
+        assert len(copies) % group == 0, (name, len(copies))
