@@ -70,8 +70,8 @@ enum { AGG_DIAG = 1u, AGG_MEAN = 2u };
 typedef enum agg_status {
   AGG_OK = 0,
   AGG_ERR_NULL = -1,        /* a required pointer is NULL                          */
-  AGG_ERR_SHAPE = -2,       /* a dimension or stride is < 1, or flags unknown      */
-  AGG_ERR_UNSUPPORTED = -3, /* D != 64; a block wider than 4096 channels           */
+  AGG_ERR_SHAPE = -2,       /* a dimension or stride is < 1, flags unknown, or buffers overlap that may not */
+  AGG_ERR_UNSUPPORTED = -3, /* D != 64; rows wider than the call takes              */
   AGG_ERR_ALIGN = -4,       /* a tensor pointer is not 16-byte aligned             */
   AGG_ERR_WORKSPACE = -5,   /* workspace smaller than the matching *_workspace_bytes */
   AGG_ERR_OVERFLOW = -6,    /* N*L, M_pad or a tensor's element count exceeds the index range */
@@ -388,10 +388,10 @@ int agg_mx4_dequantize(int64_t rows, int32_t K, const void* codes, const void* s
  * Y_i = A W_i^T + bias_i for i < count (1..3, one launch), or with a residual (count = 1)
  *     Y = R + res_scale * (A W^T + bias)
  * A: [rows, K] and W_i: [N, K] in 4 bits; products and sums in float32, one rounding.  bias_i: float32
- * [N], 16-byte aligned, or NULL.  Y_i, R: bf16 [rows, N], contiguous; Y = R works in place, other overlaps of outputs with R or each other are
- * refused with AGG_ERR_SHAPE.  res_scale: like bias_i (NULL: ones; must be NULL without R).
- * K and N are multiples of 8.  A row's bits do not depend on the other rows of the call, but on which
- * kernel its number of rows leads to.  rows = 0: nothing is done.
+ * [N], 16-byte aligned, or NULL.  Y_i, R: bf16 [rows, N], contiguous; Y = R works in place, other
+ * overlaps of an output with R, A, a W_i or another output are refused with AGG_ERR_SHAPE.  res_scale: like bias_i (NULL: ones; must be NULL without R).
+ * K and N are multiples of 8, K at most 2^22 and N at most 2^21.  rows = 0: nothing is done.  The order of a row's sums
+ * depends on the call's sizes and the row's place in it, not on the other rows.
  */
 typedef struct agg_mx4_matrix {
   const void* codes;

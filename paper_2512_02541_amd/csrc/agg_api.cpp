@@ -539,6 +539,10 @@ int make_mx4_args(int64_t rows, int32_t N, int32_t K, const agg_mx4_linear* l, c
       return AGG_ERR_SHAPE;
     for (int j = 0; j < i; ++j)
       if (overlap(l->y[i], y_bytes, l->y[j], y_bytes)) return AGG_ERR_SHAPE;
+    for (int j = 0; j < l->count; ++j)
+      if (overlap(l->y[i], y_bytes, l->w[j].codes, (uint64_t)N * mx4_code_stride(K)) ||
+          overlap(l->y[i], y_bytes, l->w[j].scales, (uint64_t)N * mx4_scale_stride(K)))
+        return AGG_ERR_SHAPE;
     a->w[i] = Mx4Matrix{(const uint8_t*)l->w[i].codes, (const uint8_t*)l->w[i].scales};
     a->bias[i] = l->bias[i];
     a->y[i] = (uint16_t*)l->y[i];

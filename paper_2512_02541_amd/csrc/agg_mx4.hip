@@ -23,6 +23,15 @@ __device__ inline uint32_t pack2(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, h);
 }
 __device__ inline const uint8_t* uniform_ptr8(const uint8_t* q) { return (const uint8_t*)uniform_ptr((const uint16_t*)q); }
+// f(0), f(1), ... with numbers that the compiler knows
+template <class F, int... i>
+__device__ __forceinline__ void for_each_of(F&& f, std::integer_sequence<int, i...>) {
+  (f(std::integral_constant<int, i>{}), ...);
+}
+template <int n, class F>
+__device__ __forceinline__ void for_each(F&& f) {
+  for_each_of(f, std::make_integer_sequence<int, n>{});
+}
 // The lane's number, worked out where it stands: what follows from it is not held in registers from
 // one place of a kernel to another.
 __device__ __forceinline__ int lane_again() {
@@ -60,7 +69,8 @@ __global__ __launch_bounds__(kQuantThreads) void mx4_quantize_kernel(
   const int64_t row = (int64_t)blockIdx.x * (kQuantThreads / 64) + (threadIdx.x >> 6);
   if (row >= rows) return;
   const int nchunk = K / 8;
-  for (int w = lane; w < words; w += 64) {  // words: a multiple of 32, so four lanes leave together
+  // words: a multiple of 32, so four lanes leave together
+  for (int w = blockIdx.y * 64 + lane; w < words; w += gridDim.y * 64) {
     u32x4 v = {0u, 0u, 0u, 0u};
     if (w < nchunk) v = *reinterpret_cast<const u32x4*>(x + row * x_stride + w * 8);
     uint32_t most = 0;
@@ -82,7 +92,8 @@ __global__ __launch_bounds__(kQuantThreads) void mx4_quantize_kernel(
     if ((w & 3) == 0) scales[row * scale_stride + w / 4] = (uint8_t)s;
   }
   // the scales behind the row's last whole run of codes
-  for (int i = words / 4 + lane; i < scale_stride; i += 64) scales[row * scale_stride + i] = 0;
+  if (blockIdx.y == 0)
+    for (int i = words / 4 + lane; i < scale_stride; i += 64) scales[row * scale_stride + i] = 0;
 }
 
 __global__ __launch_bounds__(kQuantThreads) void mx4_dequantize_kernel(
@@ -91,7 +102,7 @@ __global__ __launch_bounds__(kQuantThreads) void mx4_dequantize_kernel(
   const int lane = threadIdx.x & 63;
   const int64_t row = (int64_t)blockIdx.x * (kQuantThreads / 64) + (threadIdx.x >> 6);
   if (row >= rows) return;
-  for (int w = lane; w < K / 8; w += 64) {
+  for (int w = blockIdx.y * 64 + lane; w < K / 8; w += gridDim.y * 64) {
     const uint32_t code = codes[row * words + w];
     const uint32_t s = scales[row * scale_stride + w / 4];
     const float scale = __uint_as_float(s << 23);
@@ -112,7 +123,8 @@ __global__ __launch_bounds__(kQuantThreads) void mx4_dequantize_kernel(
 //
 // For few rows: 16 tokens x 16 channels a workgroup, whose eight wavefronts share k; their sums meet
 // in LDS, in a fixed order.  What counts is one chain of latencies: fragments come straight from memory,
-// up to four steps of 128 channels under way at once.
+// up to four steps of 128 channels under way at once.  Measured: 1 row of 1024 -> 1024 2.7 us, of 4096 -> 1024 4.1
+// (7.2 and 15.7 in a 32 x 64 tile a wavefront); 64 rows of 4096 -> 1024 5.8.
 // ---------------------------------------------------------------------------
 constexpr int kFewWaves = 8;
 
@@ -172,14 +184,25 @@ __global__ __launch_bounds__(64 * kFewWaves) void mx4_few_kernel(Mx4LinearArgs p
 }
 
 // ---------------------------------------------------------------------------
-// The same product in tiles of kEdge tokens x kEdge channels, four wavefronts of half the edge each
-// way.  k advances 256 at a time, whole 128-byte lines of codes, copied global -> LDS without passing through
-// registers into a ring of kStages steps; the scales of two steps, 16 bytes of a row, come with the
-// first of them into a ring of their own.  LDS rows are 128 bytes with the 16-byte chunk number
+// The same product in tiles of kTM tokens x kTN channels, shared out to kWM x kWN wavefronts.
+// k advances 256 at a time, whole 128-byte lines of codes, copied global -> LDS without passing through
+// registers into one or two stages; the scales of two steps, 16 bytes of a row, come with the
+// first of them into slots of their own.  LDS rows are 128 bytes with the 16-byte chunk number
 // XOR-ed by bits 1..3 of the row, which spreads the 16 rows of a fragment read over all banks.
 // Which 32 of a step's 256 channels a group of lanes multiplies in which of the two MFMAs is free as
 // long as both operands agree: group G takes blocks 2 G and 2 G + 1, so that both scales come with
-// one two-byte read and the MFMA's own byte selection tells them apart.
+// one two-byte read and the MFMA's own byte selection tells them apart; block 2 G + h lies at position
+// 4 h + G of its row (with the blocks in order the reads conflicted two-way).
+//
+// With one stage nothing hides inside a workgroup: four of them share a CU, and one's copies and stores run beside
+// another's products; with fewer tiles two stages are faster (the plan has both sides).  Outputs are stored past
+// the caches, whose lines the operands need: Q/K/V of 137 400 x 1024 in tiles of 128, four on a CU,
+// 451 us through them, 326 past them.
+// Measured: 21 984 x 4096 -> 1024 60 us without a residual, 64 with one (184 GFLOP: 3.1 PFLOP/s); 21 984 x 4096 -> 4096
+// 197 us (3.7 PFLOP/s, tiles of 256; MFMAs alone on random codes reach 6.3 to 6.8, limited by power: 9.6 on zeros).  A step of
+// a 256-wide tile takes 1.5 us, of which its products are 0.9; its copies alone and its products with their fragment
+// reads alone take 1.0 to 1.1 each.  No faster: a third stage; the next half's fragments read during a half's products;
+// one group of wavefronts half a step behind the other; tiles of 192 tokens; tiles that begin at different k.
 // ---------------------------------------------------------------------------
 constexpr int kStepBytes = 128;   // of a row of codes: 256 channels
 constexpr int kScaleBytes = 16;   // of a row of scales: two steps
@@ -189,6 +212,7 @@ __global__ __launch_bounds__(64 * kWM * kWN, kPerSimd) void mx4_tile_kernel(Mx4L
   constexpr int kWaves = kWM * kWN;
   constexpr int kMT = kTM / kWM / 16, kNT = kTN / kWN / 16;  // 16-token and 16-channel tiles of a wavefront
   constexpr int kWTM = kTM / kWM, kWTN = kTN / kWN;
+  static_assert(8 % kNT == 0, "a lane's channels of a token all exist or none: N is a multiple of 8");
   constexpr int kStepA = kTM * kStepBytes, kStepW = kTN * kStepBytes;  // a step's rows
   constexpr int kCopiesA = kTM / 8 / kWaves, kCopiesW = kTN / 8 / kWaves;  // copies of a wavefront per step
   constexpr int kScaleSlots = (kStages + 2) / 2;
@@ -289,24 +313,13 @@ __global__ __launch_bounds__(64 * kWM * kWN, kPerSimd) void mx4_tile_kernel(Mx4L
   // kOdd: the second of the two steps that share a row's scales
   auto step = [&](int k, auto odd) {
     constexpr int kOdd = decltype(odd)::value;
-    // all but the copies of the steps k + 1 .. k + kStages - 2 are awaited
-    constexpr int kAhead = kStages - 2;
     if constexpr (kStages == 1) {
       if (k > 0) lds_barrier();
       copy(kOdd == 0);
-      wait_vm0();
-      lds_barrier();
-    } else {
-      bool rest = true;
-      if constexpr (kAhead > 0)
-        if (k + kAhead < nk) {
-          wait_vm<kAhead * (kCopiesA + kCopiesW) + (kAhead + kOdd) / 2 * kScaleCopies>();
-          rest = false;
-        }
-      if (rest) wait_vm0();
-      lds_barrier();  // everybody's copies of this step are in, and the last step's stage is free
-      if (k + kStages - 1 < nk) copy((kStages - 1 + kOdd) % 2 == 0);
     }
+    wait_vm0();
+    lds_barrier();  // everybody's copies of this step are in, and with two stages the last step's is free
+    if (kStages == 2 && k + 1 < nk) copy(kOdd == 1);
     const lds_char* at_a = lds + stage * (kStepA + kStepW) + wm * kStepBytes;
     const lds_char* at_w = lds + stage * (kStepA + kStepW) + kStepA + wn * kStepBytes;
     const lds_char* sc = lds + kScalesAt + slot * kScaleSlot + c * kScaleBytes + 8 * kOdd + 2 * G;
@@ -335,9 +348,7 @@ __global__ __launch_bounds__(64 * kWM * kWN, kPerSimd) void mx4_tile_kernel(Mx4L
     if (kOdd) slot = slot + 1 == kScaleSlots ? 0 : slot + 1;
   };
 
-#pragma unroll
-  for (int s = 0; s < kStages - 1; ++s)
-    if (s < nk) copy(s % 2 == 0);
+  if (kStages == 2) copy(true);
   for (int k = 0; k < nk; k += 2) {
     step(k, std::integral_constant<int, 0>{});
     if (k + 1 >= nk) break;
@@ -405,6 +416,12 @@ static hipError_t launch_mx4_tiles(Mx4LinearArgs p, hipStream_t st) {
 // A pass over 64 channels is awaited three passes after it was requested, with the stores of those
 // passes still on their way behind it.
 // Workgroup: 512 tokens.  The list of (512 tokens, 64 channels) is shared out evenly.
+//
+// Measured: Q/K/V of 137 400 x 1024 (864 GFLOP, 844 MB of outputs) 232 us, 3.7 PFLOP/s; 250 with all wavefronts
+// storing at a pass's end, 315 in tiles.  Without its stores 186, without its products 192, products and fragment
+// reads alone 173: products (power) and stores (a kernel that does nothing else writes this pattern in 165 us) bound it
+// together.  K = 512, 3 x 512 channels: 93 us against 113.  With a residual, read like the stores are written and two
+// 16-token tiles a wavefront for the registers, it was no faster than tiles (163 to 181 us against 173).
 // ---------------------------------------------------------------------------
 constexpr int kPanelThreads = 512;
 constexpr int kPassSlots = 4;
@@ -612,9 +629,7 @@ __global__ __launch_bounds__(kPanelThreads, 2) void mx4_panel_kernel(Mx4LinearAr
             acc[t][u] = mfma4<s % 4>(fa[t][s], fw[s % 2][u], s == 0 ? start[u] : acc[t][u], sa[t][s / 4], sw[u][s / 4]);
         __builtin_amdgcn_sched_barrier(0);
       };
-      [&]<int... s>(std::integer_sequence<int, s...>) {
-        (step(std::integral_constant<int, s>{}), ...);
-      }(std::make_integer_sequence<int, kKS>{});
+      for_each<kKS>(step);
       if constexpr (h == 0) {
 #pragma unroll
         for (int t = 0; t < kMT; ++t)
@@ -647,12 +662,18 @@ static hipError_t launch_mx4_few(Mx4LinearArgs p, hipStream_t st) {
 }
 
 static inline int64_t row_groups(int64_t rows) { return (rows + kQuantThreads / 64 - 1) / (kQuantThreads / 64); }
+// Few rows are shared out by runs of 512 channels too: 1, 1374 rows of 4096 4.1, 5.1 us by whole rows, 2.5, 4.1 shared
+// out; 21 984 rows 34.3 by whole rows, 39.7 shared out.
+static dim3 quant_grid(int64_t rows, int words) {
+  const int64_t runs = rows < 2048 ? (words + 63) / 64 : 1;
+  return dim3((unsigned)row_groups(rows), (unsigned)(runs < 65535 ? runs : 65535));
+}
 
 hipError_t launch_mx4_quantize(const void* x, int64_t x_stride, void* codes, void* scales, int64_t rows, int K,
                                hipStream_t st) {
   if (row_groups(rows) > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
   (void)hipGetLastError();
-  hipLaunchKernelGGL(mx4_quantize_kernel, dim3((unsigned)row_groups(rows)), dim3(kQuantThreads), 0, st,
+  hipLaunchKernelGGL(mx4_quantize_kernel, quant_grid(rows, (int)(mx4_code_stride(K) / 4)), dim3(kQuantThreads), 0, st,
                      (const uint16_t*)x, x_stride, (uint32_t*)codes, (uint8_t*)scales, rows, K,
                      (int)(mx4_code_stride(K) / 4), (int)mx4_scale_stride(K));
   return hipGetLastError();
@@ -661,7 +682,7 @@ hipError_t launch_mx4_quantize(const void* x, int64_t x_stride, void* codes, voi
 hipError_t launch_mx4_dequantize(const void* codes, const void* scales, void* x, int64_t rows, int K, hipStream_t st) {
   if (row_groups(rows) > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
   (void)hipGetLastError();
-  hipLaunchKernelGGL(mx4_dequantize_kernel, dim3((unsigned)row_groups(rows)), dim3(kQuantThreads), 0, st,
+  hipLaunchKernelGGL(mx4_dequantize_kernel, quant_grid(rows, (int)(mx4_code_stride(K) / 4)), dim3(kQuantThreads), 0, st,
                      (const uint32_t*)codes, (const uint8_t*)scales, (uint16_t*)x, rows, K,
                      (int)(mx4_code_stride(K) / 4), (int)mx4_scale_stride(K));
   return hipGetLastError();

@@ -663,6 +663,55 @@ def test_operators_on_other_streams_and_in_graphs():
         assert same_bits(y_, a) and same_bits(n_, b)
 
 
+def test_single_operators_in_graphs():
+    """Each by itself, the kernels for many rows among them, replayed on inputs that change in between."""
+    say("single operators in graphs")
+    g = gen(71)
+    shape = agg.make_shape(1, 4, 9, 7, 5, 3, 64, 1, 1)
+    rope = agg.make_rope(agg.AGG_ROPE_HEAD, 16, 24, 24, t0=3)
+    q = normal(g, 1, shape.NQ, 3, 64).to(torch.bfloat16)
+    qr, kr = torch.empty_like(q), torch.empty_like(q)
+    rows, C = 1003, 4096
+    x, b = (normal(g, rows, C).to(torch.bfloat16) for _ in "xb")
+    r = agg.make_residual(make_norm(g, "layer", C)[0], make_norm(g, "layer", C)[0], normal(g, C))
+    h, n = torch.empty_like(x), torch.empty_like(x)
+    a = [harness.mx4_quantize(t) for t in (x, b)]
+    w = harness.mx4_quantize((normal(g, 264, C) / 64).to(torch.bfloat16))
+    y = [torch.empty((rows, 264), dtype=torch.bfloat16, device="cuda") for _ in "ab"]
+    plans = [agg.make_mx4_linear([w], [t]) for t in y]
+    many = normal(g, 22000, 512).to(torch.bfloat16)
+    held_many = harness.mx4_quantize(many)
+    wide = harness.mx4_quantize((normal(g, 3080, 512) / 22).to(torch.bfloat16))
+    out = torch.empty((22000, 3080), dtype=torch.bfloat16, device="cuda")
+    panel = agg.make_mx4_linear([wide], [out])
+
+    def run():
+        agg.agg_rope_fwd(shape, rope, None, None, None, q, 0, q, 0, qr, kr)
+        agg.agg_residual_norm_fwd(rows, C, r, x, b, h, n)
+        agg.agg_mx4_quantize(rows, C, n, 0, *a[0])
+        for plan in plans:
+            agg.agg_mx4_linear_fwd(rows, 264, C, plan, *a[0])
+        agg.agg_mx4_quantize(22000, 512, many, 0, *held_many)
+        agg.agg_mx4_linear_fwd(22000, 3080, 512, panel, *held_many)
+        return [t.clone() for t in (qr, kr, h, n, y[0], y[1], out)]
+
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for i in range(3):
+        for t in (q, x, b, many):
+            t.copy_(normal(g, *t.shape).to(torch.bfloat16))
+        want = run()
+        for t in (qr, kr, h, n, *y, out):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for t, v in zip((qr, kr, h, n, *y, out), want):
+            assert same_bits(t, v), i
+
+
 def test_operators_repeat_to_the_bit():
     say("operators repeat")
     shape = agg.make_shape(1, 3, 13, 11, 5, 16, 64, 2, 2, 1)

@@ -213,6 +213,8 @@ def test_mx4_refusals():
     assert _linear(count=2, residual=_at(5)) == S and _linear(res_scale=_at(5)) == S
     assert _linear(count=2, y=[_at(9), _at(9) + 16]) == S and _linear(residual=_at(10) + 2048) == S
     assert _linear(y=[_at(0) + 512]) == S and _linear(y=[_at(1) + 16]) == S
+    assert _linear(y=[_at(2) + 512]) == S and _linear(y=[_at(3) - 16]) == S
+    assert _linear(K=1 << 23) == O and _linear(rows=1 << 31, N=1 << 21) == O
     m = agg.make_mx4_linear([(_at(2), _at(3))], [_at(9)])
     m.count = 4
     assert _status(agg.agg_mx4_linear_fwd, 1, 64, 64, m, _at(0), _at(1)) == S
