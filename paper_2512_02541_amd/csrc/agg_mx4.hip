@@ -5,6 +5,7 @@
 #include "agg_internal.h"
 #include "agg_lds_copy.h"
 #include "agg_mx4_plan.h"
+#include "agg_stream.h"
 
 namespace agg {
 
@@ -58,10 +59,12 @@ __device__ inline float bf16_of(uint32_t bits) { return __uint_as_float(bits << 
 // NaN and infinity last), and its exponent field minus 2 is the scale's byte; the conversion
 // instruction divides by the scale and rounds to the nearest, ties to even, saturating.  (For a
 // scale byte of 0 the float with exponent field 0 stands for 2^-127: all 255 scales and all finite bf16
-// values were compared with the definition.)  One wavefront per row; HBM-bound.
+// values were compared with the definition.)  One wavefront per row; HBM-bound: 137 400 rows of 1024 and back
+// 109 us (712 MB, the codes counted twice), 134 with ordinary accesses to the bf16 tensors.
 // ---------------------------------------------------------------------------
 constexpr int kQuantThreads = 256;
 
+template <bool kStream>
 __global__ __launch_bounds__(kQuantThreads) void mx4_quantize_kernel(
     const uint16_t* __restrict__ x, int64_t x_stride, uint32_t* __restrict__ codes,
     uint8_t* __restrict__ scales, int64_t rows, int K, int words, int scale_stride) {
@@ -72,7 +75,7 @@ __global__ __launch_bounds__(kQuantThreads) void mx4_quantize_kernel(
   // words: a multiple of 32, so four lanes leave together
   for (int w = blockIdx.y * 64 + lane; w < words; w += gridDim.y * 64) {
     u32x4 v = {0u, 0u, 0u, 0u};
-    if (w < nchunk) v = *reinterpret_cast<const u32x4*>(x + row * x_stride + w * 8);
+    if (w < nchunk) v = load16<kStream>(x + row * x_stride + w * 8);
     uint32_t most = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) most = max(most, max(v[i] & 0x7FFFu, (v[i] >> 16) & 0x7FFFu));
@@ -96,6 +99,7 @@ __global__ __launch_bounds__(kQuantThreads) void mx4_quantize_kernel(
     for (int i = words / 4 + lane; i < scale_stride; i += 64) scales[row * scale_stride + i] = 0;
 }
 
+template <bool kStream>
 __global__ __launch_bounds__(kQuantThreads) void mx4_dequantize_kernel(
     const uint32_t* __restrict__ codes, const uint8_t* __restrict__ scales, uint16_t* __restrict__ x,
     int64_t rows, int K, int words, int scale_stride) {
@@ -112,7 +116,7 @@ __global__ __launch_bounds__(kQuantThreads) void mx4_dequantize_kernel(
     v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 2));
     v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 3));
     if (s == 255) v = u32x4{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};
-    *reinterpret_cast<u32x4*>(x + row * K + w * 8) = v;
+    store16<kStream>(x + row * K + w * 8, v);
   }
 }
 
@@ -673,7 +677,8 @@ hipError_t launch_mx4_quantize(const void* x, int64_t x_stride, void* codes, voi
                                hipStream_t st) {
   if (row_groups(rows) > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
   (void)hipGetLastError();
-  hipLaunchKernelGGL(mx4_quantize_kernel, quant_grid(rows, (int)(mx4_code_stride(K) / 4)), dim3(kQuantThreads), 0, st,
+  const auto kernel = streams(rows * K * 2) ? mx4_quantize_kernel<true> : mx4_quantize_kernel<false>;
+  hipLaunchKernelGGL(kernel, quant_grid(rows, (int)(mx4_code_stride(K) / 4)), dim3(kQuantThreads), 0, st,
                      (const uint16_t*)x, x_stride, (uint32_t*)codes, (uint8_t*)scales, rows, K,
                      (int)(mx4_code_stride(K) / 4), (int)mx4_scale_stride(K));
   return hipGetLastError();
@@ -682,7 +687,8 @@ hipError_t launch_mx4_quantize(const void* x, int64_t x_stride, void* codes, voi
 hipError_t launch_mx4_dequantize(const void* codes, const void* scales, void* x, int64_t rows, int K, hipStream_t st) {
   if (row_groups(rows) > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
   (void)hipGetLastError();
-  hipLaunchKernelGGL(mx4_dequantize_kernel, quant_grid(rows, (int)(mx4_code_stride(K) / 4)), dim3(kQuantThreads), 0, st,
+  const auto kernel = streams(rows * K * 2) ? mx4_dequantize_kernel<true> : mx4_dequantize_kernel<false>;
+  hipLaunchKernelGGL(kernel, quant_grid(rows, (int)(mx4_code_stride(K) / 4)), dim3(kQuantThreads), 0, st,
                      (const uint32_t*)codes, (const uint8_t*)scales, (uint16_t*)x, rows, K,
                      (int)(mx4_code_stride(K) / 4), (int)mx4_scale_stride(K));
   return hipGetLastError();

@@ -3,6 +3,7 @@
 // whose bound is HBM: every row is read once, held in registers in float32 and written once.
 #include "agg_internal.h"
 #include "agg_lds_copy.h"
+#include "agg_stream.h"
 
 namespace agg {
 
@@ -234,7 +235,7 @@ hipError_t launch_rope(const RopeArgs& args, hipStream_t st) {
 // from row to row, and the next row is requested before the present one is worked on.
 // Rows of up to 1024 channels: one wavefront each, kPer 16-byte chunks a lane.  Few longer ones: the
 // whole workgroup, of as many wavefronts as the row fills, whose sums meet in LDS.
-// HBM-bound: 21 984 rows of 1024 with layer scale and LayerNorm 29 to 31 us (180 MB), 137 400 rows 230 (4.9 TB/s); one row 2.4 us.
+// HBM-bound: 21 984 rows of 1024 with layer scale and LayerNorm 28 to 29 us (180 MB), 137 400 rows 200 (5.6 TB/s); one row 2.4 us.
 // ---------------------------------------------------------------------------
 namespace {
 
@@ -289,7 +290,7 @@ struct SeamRow {
 
 }  // namespace
 
-template <int kPer, bool kAcross>
+template <int kPer, bool kAcross, bool kStream>
 __global__ __launch_bounds__(kAcross ? 512 : 256) void seam_kernel(SeamArgs a) {
   __shared__ float slots[2][8];
   const int waves = blockDim.x >> 6;
@@ -320,8 +321,8 @@ __global__ __launch_bounds__(kAcross ? 512 : 256) void seam_kernel(SeamArgs a) {
   auto request = [&](int64_t row) {
 #pragma unroll
     for (int c = 0; c < kPer; ++c) {
-      xr[c] = *reinterpret_cast<const u32x4*>(a.x + row * a.C + off[c]);
-      if (a.branch) br[c] = *reinterpret_cast<const u32x4*>(a.branch + row * a.C + off[c]);
+      xr[c] = load16<kStream>(a.x + row * a.C + off[c]);
+      if (a.branch) br[c] = load16<kStream>(a.branch + row * a.C + off[c]);
       if (a.gate)  // rows < 2^31 and gate_rows <= 2^31
         gr[c] = *reinterpret_cast<const u32x4*>(a.gate + (int64_t)((uint32_t)row / (uint32_t)a.gate_rows) * a.C + off[c]);
     }
@@ -368,13 +369,13 @@ __global__ __launch_bounds__(kAcross ? 512 : 256) void seam_kernel(SeamArgs a) {
     if (a.h) {
 #pragma unroll
       for (int c = 0; c < kPer; ++c)
-        if (has[c]) *reinterpret_cast<u32x4*>(a.h + row * a.C + off[c]) = pack8(r.v[c]);
+        if (has[c]) store16<true>(a.h + row * a.C + off[c], pack8(r.v[c]));
     }
     if (a.pre.kind != AGG_NORM_NONE) {
       r.norm(a.pre, pre, has, inv_c, slots, turn, waves);
 #pragma unroll
       for (int c = 0; c < kPer; ++c)
-        if (has[c]) *reinterpret_cast<u32x4*>(a.n + row * a.C + off[c]) = pack8(r.v[c]);
+        if (has[c]) store16<kStream>(a.n + row * a.C + off[c], pack8(r.v[c]));
     }
   }
 }
@@ -389,7 +390,7 @@ __global__ __launch_bounds__(kAcross ? 512 : 256) void seam_kernel(SeamArgs a) {
 // ---------------------------------------------------------------------------
 constexpr int kLongThreads = 256;
 
-template <int kChunks>
+template <int kChunks, bool kStream>
 __global__ __launch_bounds__(kLongThreads, kChunks <= 4 ? 4 : kChunks <= 6 ? 3 : 2) void seam_long_kernel(SeamArgs a) {
   extern __shared__ __align__(16) float params[];
   const int lane = threadIdx.x & 63;
@@ -455,9 +456,9 @@ __global__ __launch_bounds__(kLongThreads, kChunks <= 4 ? 4 : kChunks <= 6 ? 3 :
     float v[kChunks][8];
 #pragma unroll
     for (int c = 0; c < kChunks; ++c) {
-      xr[c] = *reinterpret_cast<const u32x4*>(a.x + row * a.C + at(c));
+      xr[c] = load16<kStream>(a.x + row * a.C + at(c));
       u32x4 br = {0u, 0u, 0u, 0u};
-      if (a.branch) br = *reinterpret_cast<const u32x4*>(a.branch + row * a.C + at(c));
+      if (a.branch) br = load16<kStream>(a.branch + row * a.C + at(c));
       if (a.gate)  // rows < 2^31 and gate_rows <= 2^31
         gr[c] = *reinterpret_cast<const u32x4*>(a.gate + (int64_t)((uint32_t)row / (uint32_t)a.gate_rows) * a.C + at(c));
       unpack8(br, v[c]);
@@ -481,26 +482,26 @@ __global__ __launch_bounds__(kLongThreads, kChunks <= 4 ? 4 : kChunks <= 6 ? 3 :
       unpack8(xr[c], f);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[c][i] = has(c) ? v[c][i] + f[i] : 0.f;
-      if (a.h && has(c)) *reinterpret_cast<u32x4*>(a.h + row * a.C + at(c)) = pack8(v[c]);
+      if (a.h && has(c)) store16<true>(a.h + row * a.C + at(c), pack8(v[c]));
     }
     if (a.pre.kind != AGG_NORM_NONE) {
       norm(v, a.pre, place[3], place[4]);
 #pragma unroll
       for (int c = 0; c < kChunks; ++c)
-        if (has(c)) *reinterpret_cast<u32x4*>(a.n + row * a.C + at(c)) = pack8(v[c]);
+        if (has(c)) store16<kStream>(a.n + row * a.C + at(c), pack8(v[c]));
     }
   }
 }
 
-template <int kPer, bool kAcross>
+template <int kPer, bool kAcross, bool kStream>
 static hipError_t launch_seam_rows(const SeamArgs& a, int threads, hipStream_t st) {
   const int64_t groups = kAcross ? a.rows : (a.rows + 3) / 4;
   const int64_t most = 256 * 2048 / threads;  // as many threads as the CUs hold
-  hipLaunchKernelGGL((seam_kernel<kPer, kAcross>), dim3((unsigned)(groups < most ? groups : most)), dim3(threads), 0, st, a);
+  hipLaunchKernelGGL((seam_kernel<kPer, kAcross, kStream>), dim3((unsigned)(groups < most ? groups : most)), dim3(threads), 0, st, a);
   return hipGetLastError();
 }
 
-template <int kChunks>
+template <int kChunks, bool kStream>
 static hipError_t launch_seam_long(const SeamArgs& a, hipStream_t st) {
   const float* const from[5] = {a.post.gamma, a.post.beta, a.scale, a.pre.gamma, a.pre.beta};
   int held = 0;
@@ -510,13 +511,28 @@ static hipError_t launch_seam_long(const SeamArgs& a, hipStream_t st) {
   const int fit = bytes ? 160 * 1024 / bytes : 8;
   const int64_t most = 256 * (kChunks <= 4 ? min(fit, 4) : kChunks <= 6 ? min(fit, 3) : 2);
   if (bytes > 64 * 1024) {
-    const hipError_t e = hipFuncSetAttribute((const void*)seam_long_kernel<kChunks>,
+    const hipError_t e = hipFuncSetAttribute((const void*)seam_long_kernel<kChunks, kStream>,
                                              hipFuncAttributeMaxDynamicSharedMemorySize, 80 * 1024);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(seam_long_kernel<kChunks>, dim3((unsigned)(groups < most ? groups : most)), dim3(kLongThreads),
+  hipLaunchKernelGGL((seam_long_kernel<kChunks, kStream>), dim3((unsigned)(groups < most ? groups : most)), dim3(kLongThreads),
                      bytes, st, a);
   return hipGetLastError();
+}
+
+template <bool kStream>
+static hipError_t launch_seam_many(const SeamArgs& a, int waves, hipStream_t st) {
+  switch (waves) {
+    case 1: return launch_seam_rows<1, false, kStream>(a, 256, st);
+    case 2: return launch_seam_rows<2, false, kStream>(a, 256, st);
+    case 3: return launch_seam_long<3, kStream>(a, st);
+    case 4: return launch_seam_long<4, kStream>(a, st);
+    case 5: return launch_seam_long<5, kStream>(a, st);
+    case 6: return launch_seam_long<6, kStream>(a, st);
+    case 7: return launch_seam_long<7, kStream>(a, st);
+    case 8: return launch_seam_long<8, kStream>(a, st);
+  }
+  return launch_seam_rows<2, true, kStream>(a, 512, st);
 }
 
 hipError_t launch_seam(const SeamArgs& args, hipStream_t st) {
@@ -526,20 +542,10 @@ hipError_t launch_seam(const SeamArgs& args, hipStream_t st) {
   if (a.pre.kind == AGG_NORM_NONE) a.pre.gamma = a.pre.beta = nullptr;
   const int waves = (a.C / 8 + 63) / 64;  // one chunk a thread
   (void)hipGetLastError();
-  if (waves == 1) return launch_seam_rows<1, false>(a, 256, st);
-  if (waves == 2) return launch_seam_rows<2, false>(a, 256, st);
-  if (waves > 8) return launch_seam_rows<2, true>(a, 512, st);
   // Few rows: the whole workgroup on one of them. us for 1, 512, 1000 rows of 2112 channels with every part:
   // 3.8, 5.1, 10.0 against 5.7, 7.0, 8.0 a wavefront each; 1, 768 rows of 4096: 3.7, 7.9 against 7.5, 10.4
-  if (a.rows <= 896) return launch_seam_rows<1, true>(a, 64 * waves, st);
-  switch (waves) {
-    case 3: return launch_seam_long<3>(a, st);
-    case 4: return launch_seam_long<4>(a, st);
-    case 5: return launch_seam_long<5>(a, st);
-    case 6: return launch_seam_long<6>(a, st);
-    case 7: return launch_seam_long<7>(a, st);
-  }
-  return launch_seam_long<8>(a, st);
+  if (waves > 2 && waves <= 8 && a.rows <= 896) return launch_seam_rows<1, true, false>(a, 64 * waves, st);
+  return streams(a.rows * a.C * 2) ? launch_seam_many<true>(a, waves, st) : launch_seam_many<false>(a, waves, st);
 }
 
 }  // namespace agg

@@ -712,6 +712,34 @@ def test_single_operators_in_graphs():
             assert same_bits(t, v), i
 
 
+@pytest.mark.parametrize("rows, C", [(70003, 488), (35001, 1000), (23003, 1536), (8201, 4104)])
+def test_large_tensors_equal_their_parts(rows, C):
+    """Tensors of more than 64 MiB are read and written past the caches: the same bits as in parts below that."""
+    say("large tensors", rows, C)
+    g = gen(44)
+    x, b = (normal(g, rows, C).to(torch.bfloat16) for _ in "xb")
+    gate = normal(g, (rows + 999) // 1000, C).to(torch.bfloat16)
+    post, pre = make_norm(g, "rms", C)[0], make_norm(g, "layer", C)[0]
+    scale = normal(g, C)
+    r = agg.make_residual(post=post, pre=pre, scale=scale, gate=gate, gate_rows=1000)
+    assert rows * C * 2 > 64 << 20 and rows % 1000
+    h, n = harness.residual_forward(r, x, b)
+    codes, scales = harness.mx4_quantize(n)
+    back = harness.mx4_dequantize((codes, scales), C)
+    for i in range(0, rows, 20000 if C < 512 else 5000):
+        part = slice(i, min(i + (20000 if C < 512 else 5000), rows))
+        own = agg.make_residual(post=post, pre=pre, scale=scale, gate=gate[i // 1000:].contiguous(), gate_rows=1000)
+        hp, np_ = harness.residual_forward(own, x[part].contiguous(), b[part].contiguous())
+        assert same_bits(hp, h[part]) and same_bits(np_, n[part]), i
+        cp, sp = harness.mx4_quantize(np_)
+        assert torch.equal(cp, codes[part]) and torch.equal(sp, scales[part]), i
+        assert same_bits(harness.mx4_dequantize((cp, sp), C), back[part]), i
+    # and in place
+    a, c = x.clone(), b.clone()
+    agg.agg_residual_norm_fwd(rows, C, r, a, c, a, c)
+    assert same_bits(a, h) and same_bits(c, n)
+
+
 def test_operators_repeat_to_the_bit():
     say("operators repeat")
     shape = agg.make_shape(1, 3, 13, 11, 5, 16, 64, 2, 2, 1)
