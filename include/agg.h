@@ -195,7 +195,8 @@ int agg_frame_attn_fwd(const agg_shape* shape, const void* Q, const void* K, con
  * Weights: device memory; w_*: bf16 [C, C], one row per OUTPUT channel (y = x W^T);
  * b_* (may be NULL), ln_gamma, ln_beta: float32 [C].  Q, K, V and the attention output
  * are bf16 tensors in the workspace, as in the calls above.  Rotary embeddings or
- * query/key normalisation, which the paper's text does not describe, are not applied.
+ * query/key normalisation, which the paper's text does not describe, are not applied
+ * (agg_global_block_ex_fwd below applies them).
  * C may be at most 4096 (64 heads): wider blocks return AGG_ERR_UNSUPPORTED.
  */
 typedef struct agg_block_weights {
