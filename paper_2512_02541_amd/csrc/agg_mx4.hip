@@ -665,32 +665,39 @@ static hipError_t launch_mx4_few(Mx4LinearArgs p, hipStream_t st) {
   return hipGetLastError();
 }
 
-static inline int64_t row_groups(int64_t rows) { return (rows + kQuantThreads / 64 - 1) / (kQuantThreads / 64); }
 // Few rows are shared out by runs of 512 channels too: 1, 1374 rows of 4096 4.1, 5.1 us by whole rows, 2.5, 4.1 shared
 // out; 21 984 rows 34.3 by whole rows, 39.7 shared out.
 static dim3 quant_grid(int64_t rows, int words) {
   const int64_t runs = rows < 2048 ? (words + 63) / 64 : 1;
-  return dim3((unsigned)row_groups(rows), (unsigned)(runs < 65535 ? runs : 65535));
+  return dim3((unsigned)((rows + kQuantThreads / 64 - 1) / (kQuantThreads / 64)), (unsigned)(runs < 65535 ? runs : 65535));
 }
+// rows of a launch: its threads are counted with 32 bits
+constexpr int64_t kQuantRows = (int64_t)1 << 25;
 
 hipError_t launch_mx4_quantize(const void* x, int64_t x_stride, void* codes, void* scales, int64_t rows, int K,
                                hipStream_t st) {
-  if (row_groups(rows) > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
-  (void)hipGetLastError();
+  const int words = (int)(mx4_code_stride(K) / 4), scale_stride = (int)mx4_scale_stride(K);
   const auto kernel = streams(rows * K * 2) ? mx4_quantize_kernel<true> : mx4_quantize_kernel<false>;
-  hipLaunchKernelGGL(kernel, quant_grid(rows, (int)(mx4_code_stride(K) / 4)), dim3(kQuantThreads), 0, st,
-                     (const uint16_t*)x, x_stride, (uint32_t*)codes, (uint8_t*)scales, rows, K,
-                     (int)(mx4_code_stride(K) / 4), (int)mx4_scale_stride(K));
+  (void)hipGetLastError();
+  for (int64_t first = 0; first < rows; first += kQuantRows) {
+    const int64_t here = rows - first < kQuantRows ? rows - first : kQuantRows;
+    hipLaunchKernelGGL(kernel, quant_grid(here, words), dim3(kQuantThreads), 0, st,
+                       (const uint16_t*)x + first * x_stride, x_stride, (uint32_t*)codes + first * words,
+                       (uint8_t*)scales + first * scale_stride, here, K, words, scale_stride);
+  }
   return hipGetLastError();
 }
 
 hipError_t launch_mx4_dequantize(const void* codes, const void* scales, void* x, int64_t rows, int K, hipStream_t st) {
-  if (row_groups(rows) > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
-  (void)hipGetLastError();
+  const int words = (int)(mx4_code_stride(K) / 4), scale_stride = (int)mx4_scale_stride(K);
   const auto kernel = streams(rows * K * 2) ? mx4_dequantize_kernel<true> : mx4_dequantize_kernel<false>;
-  hipLaunchKernelGGL(kernel, quant_grid(rows, (int)(mx4_code_stride(K) / 4)), dim3(kQuantThreads), 0, st,
-                     (const uint32_t*)codes, (const uint8_t*)scales, (uint16_t*)x, rows, K,
-                     (int)(mx4_code_stride(K) / 4), (int)mx4_scale_stride(K));
+  (void)hipGetLastError();
+  for (int64_t first = 0; first < rows; first += kQuantRows) {
+    const int64_t here = rows - first < kQuantRows ? rows - first : kQuantRows;
+    hipLaunchKernelGGL(kernel, quant_grid(here, words), dim3(kQuantThreads), 0, st,
+                       (const uint32_t*)codes + first * words, (const uint8_t*)scales + first * scale_stride,
+                       (uint16_t*)x + first * K, here, K, words, scale_stride);
+  }
   return hipGetLastError();
 }
 

@@ -740,6 +740,26 @@ def test_large_tensors_equal_their_parts(rows, C):
     assert same_bits(a, h) and same_bits(c, n)
 
 
+def test_more_rows_than_a_launch_counts():
+    """2^26 rows and some: more threads than a launch may have, offsets past 32 bits."""
+    say("many rows")
+    rows, K = (1 << 26) + 5, 8
+    x = torch.zeros(rows, K, device="cuda", dtype=torch.bfloat16)
+    edges = [0, (1 << 25) - 1, 1 << 25, (1 << 25) + 1, (1 << 26) - 1, 1 << 26, rows - 1]
+    x[edges] = normal(gen(45), len(edges), K).to(torch.bfloat16)
+    codes, scales = harness.mx4_quantize(x)
+    want = harness.mx4_quantize(x[edges].contiguous())
+    assert torch.equal(codes[edges], want[0]) and torch.equal(scales[edges], want[1])
+    assert int((scales[:, 0] != 0).sum()) == len(edges) and not bool(scales[:, 1:].any())
+    back = harness.mx4_dequantize((codes, scales), K)
+    assert same_bits(back[edges], harness.mx4_dequantize(want, K))
+    assert int((back != 0).any(1).sum()) == len(edges)
+    w = harness.mx4_quantize(normal(gen(46), 8, K).to(torch.bfloat16))
+    y, = harness.mx4_linear((codes, scales), [w], K)
+    few, = harness.mx4_linear(want, [w], K)
+    assert same_bits(y[edges], few)  # one step of k: the same sums in every kernel
+
+
 def test_operators_repeat_to_the_bit():
     say("operators repeat")
     shape = agg.make_shape(1, 3, 13, 11, 5, 16, 64, 2, 2, 1)
