@@ -171,7 +171,9 @@ struct RopeArgs {
   int64_t total, NQ;      // tokens of all sequences, of one
   int32_t H, L, P, n_w, t0, patch0;
   int32_t pairs;          // pairs of channels that turn, 0: none
-  int32_t tokens;         // of a wavefront's turn (set by launch_rope)
+  // set by launch_rope: tokens of a wavefront's turn, wavefronts that share its heads, 2 where queries and keys go to
+  // different ones
+  int32_t tokens, parts, ways;
   uint64_t freq[kHeadDim / 2];     // of a pair, in 2^-64 turns per position
   uint8_t axis[kHeadDim / 2];      // 0 time, 1 row, 2 column
   uint8_t first[kHeadDim / 2], second[kHeadDim / 2];  // its channels

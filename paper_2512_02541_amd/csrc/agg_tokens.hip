@@ -78,7 +78,7 @@ __device__ inline void wave_lds_fence() {
 // Bound by HBM once enough is under way: a round's rows are requested while the one before is worked on.
 // Measured (16 frames of 16 heads with a LayerNorm, 180 MB / 100 frames with RMS and given positions, 1.13 GB): 49 / 323 us
 // when rows were requested in their own round and sums went through LDS; 38 / 223 without that; 34 / 207 (5.4 TB/s) with a
-// table of cosine and signed sine per channel, whose reads stand in front of their uses.  One frame of 261 tokens 5 us.
+// table of cosine and signed sine per channel, whose reads stand in front of their uses.  One frame of 261 tokens of 8 heads 4 us.
 // ---------------------------------------------------------------------------
 constexpr int kRopeThreads = 256;
 constexpr int kRopeWaves = kRopeThreads / 64;
@@ -86,6 +86,7 @@ constexpr int kRopeMaxTokens = 8;            // of a wavefront's turn
 constexpr int kRopePairs = kHeadDim / 2;
 constexpr int kHeadStride = kHeadDim + 4;    // floats of a head in LDS: 16-byte aligned rows
 
+template <bool kShared>
 __global__ __launch_bounds__(kRopeThreads, 4) void rope_kernel(RopeArgs a) {
   __shared__ __align__(16) float heads[kRopeWaves][8][kHeadStride];
   __shared__ __align__(16) f32x2 turns[kRopeWaves][kRopeMaxTokens][kHeadDim];  // of a channel: cosine, signed sine
@@ -114,9 +115,21 @@ __global__ __launch_bounds__(kRopeThreads, 4) void rope_kernel(RopeArgs a) {
   }
   float* const head = heads[wave][group];
 
+  // kShared: several wavefronts share a turn's heads, or one takes the queries and one the keys; one turn each
+  int64_t first = (int64_t)blockIdx.x * kRopeWaves + wave;
+  int h0 = group % H, sub0 = group / H;
+  int skip = -1;  // the tensor that is another wavefront's
+  if constexpr (kShared) {
+    const uint32_t sharing = a.parts * a.ways, item = (uint32_t)first;
+    first = item / sharing;
+    const int part = (int)(item % sharing) / a.ways;
+    if (a.ways == 2) skip = ~item & 1;
+    h0 = (part * 8 + group) % H;
+    sub0 = (part * 8 + group) / H;
+  }
+  const int next = kShared ? 8 * a.parts : 8;
   const int64_t step = (int64_t)gridDim.x * kRopeWaves * a.tokens;
-  const int h0 = group % H, sub0 = group / H;
-  for (int64_t t0 = ((int64_t)blockIdx.x * kRopeWaves + wave) * a.tokens; t0 < a.total; t0 += step) {
+  for (int64_t t0 = first * a.tokens; t0 < a.total; t0 += step) {
     const int here = (int)min((int64_t)a.tokens, a.total - t0);
     // a turn's heads, eight at a time; a round's rows are requested while the one before is worked on
     int h = h0, sub = sub0;
@@ -125,7 +138,7 @@ __global__ __launch_bounds__(kRopeThreads, 4) void rope_kernel(RopeArgs a) {
       if (sub < here)
 #pragma unroll
         for (int t = 0; t < 2; ++t)
-          if (a.in[t])
+          if (a.in[t] && (!kShared || t != skip))
             ahead[t] = *reinterpret_cast<const u32x4*>(a.in[t] + (t0 + sub) * a.stride[t] + h * kHeadDim + c0);
     };
     request();
@@ -161,7 +174,7 @@ __global__ __launch_bounds__(kRopeThreads, 4) void rope_kernel(RopeArgs a) {
     while (sub < here) {
       u32x4 raw[2] = {ahead[0], ahead[1]};
       const int at_h = h, at_sub = sub;
-      h += 8;
+      h += next;
       while (h >= H) {
         h -= H;
         ++sub;
@@ -169,7 +182,7 @@ __global__ __launch_bounds__(kRopeThreads, 4) void rope_kernel(RopeArgs a) {
       request();
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        if (!a.in[t]) continue;
+        if (!a.in[t] || (kShared && t == skip)) continue;
         float x[8];
         unpack8(raw[t], x);
         const int kind = a.norm[t].kind;
@@ -223,9 +236,18 @@ hipError_t launch_rope(const RopeArgs& args, hipStream_t st) {
   // two tokens a turn fill the lanes that work out the angles; few tokens are spread over more wavefronts
   a.tokens = a.H < 4 ? kRopeMaxTokens / a.H : a.total <= 4096 ? 1 : 2;
   const int64_t turns = (a.total + a.tokens - 1) / a.tokens;
-  const int64_t groups = (turns + kRopeWaves - 1) / kRopeWaves;
+  // Few turns: a round costs a wavefront 0.6 to 1 us whatever runs beside it, so its heads are shared out, then queries and
+  // keys too, while all wavefronts still run at once (four on a SIMD).  us with a LayerNorm, shared / not: 1 token of 16
+  // heads 3.9 / 5.3, 261 of 8 4.0 / 4.4, of 16 4.3 / 5.7, 1374 of 16 6.5 / 6.9; beyond: 2748 of 16 8.8 / 7.9, 5496 12.0 / 11.5
+  constexpr int kAtOnce = 256 * 4 * 4;
+  a.parts = a.ways = 1;
+  while (a.parts * 8 < a.tokens * a.H && turns * a.parts * 2 <= kAtOnce) a.parts *= 2;
+  if (a.in[0] && a.in[1] && turns * a.parts * 2 <= kAtOnce) a.ways = 2;
+  const int64_t groups = (turns * a.parts * a.ways + kRopeWaves - 1) / kRopeWaves;
+  const dim3 grid((unsigned)(groups < 4096 ? groups : 4096));
   (void)hipGetLastError();
-  hipLaunchKernelGGL(rope_kernel, dim3((unsigned)(groups < 4096 ? groups : 4096)), dim3(kRopeThreads), 0, st, a);
+  const auto kernel = a.parts * a.ways > 1 ? rope_kernel<true> : rope_kernel<false>;
+  hipLaunchKernelGGL(kernel, grid, dim3(kRopeThreads), 0, st, a);
   return hipGetLastError();
 }
 

@@ -187,6 +187,33 @@ def test_rope_leaves_the_other_channels():
 
 
 # ---- the seam between branches -------------------------------------------------------------------
+@pytest.mark.parametrize("H", [1, 3, 8, 12, 16, 33, 64])
+@pytest.mark.parametrize("both", [True, False])
+def test_rope_shared_out_heads(H, both):
+    """However many wavefronts share a token's heads: the same bits, for few tokens as for many, in place too."""
+    say("rope shared heads", H, both)
+    g = gen(47)
+    total = 5003
+    q, k = (normal(g, 1, total, H, 64).to(torch.bfloat16) for _ in "qk")
+    pos = torch.randint(-1000, 1000, (1, total, 3), generator=g, device="cuda", dtype=torch.int32)
+    n = make_norm(g, "layer", 64)[0]
+    rope = agg.make_rope(agg.AGG_ROPE_SECTIONS, 16, 24, 20)
+
+    def run(part):
+        a, b = (t[:, part].contiguous() for t in (q, k))
+        shape = agg.make_shape(1, a.shape[1], 1, 1, 0, H, 64, 1, 1)
+        agg.agg_rope_fwd(shape, rope, n, n, pos[:, part].contiguous(), a, 0, b if both else None, 0, a,
+                         b if both else None)
+        return (a, b) if both else (a,)
+
+    whole = run(slice(0, total))
+    for first, size in ((0, 1), (7, 2), (1, 61), (100, 128), (90, 129), (0, 512), (3, 513), (5, 1024), (4, 1025), (0, 2048),
+                        (1, 2049), (907, 4096)):
+        part = slice(first, first + size)
+        for t, v in zip(run(part), whole):
+            assert same_bits(t, v[:, part]), (first, size)
+
+
 def seam_case(rows, C, post="none", pre="layer", scale=True, gate_rows=0, branch=True, want_h=True, seed=3,
               affine=True):
     g = gen(seed)
