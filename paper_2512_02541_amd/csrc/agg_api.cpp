@@ -840,13 +840,13 @@ int agg_global_block_ex_fwd(const agg_shape* shape, int mode, const agg_block_we
     if ((rc = make_mx4_args(rows, C, C, &l, codes, scales, &mx_out)) != AGG_OK) return rc;
   }
 
-  if (!o->first_done && launch_layernorm(x, w->ln_gamma, w->ln_beta, xn, rows, C, w->ln_eps, st) != hipSuccess)
-    return AGG_ERR_LAUNCH;
   if (o->mx) {
-    if (launch_mx4_quantize(first, C, codes, scales, rows, C, st) != hipSuccess ||
-        launch_mx4_linear(mx_qkv, st) != hipSuccess)
-      return AGG_ERR_LAUNCH;
+    const hipError_t e = o->first_done ? launch_mx4_quantize(o->x_norm, C, codes, scales, rows, C, st)
+                                       : launch_layernorm_mx4(x, w->ln_gamma, w->ln_beta, codes, scales, rows, C, w->ln_eps, st);
+    if (e != hipSuccess || launch_mx4_linear(mx_qkv, st) != hipSuccess) return AGG_ERR_LAUNCH;
   } else {
+    if (!o->first_done && launch_layernorm(x, w->ln_gamma, w->ln_beta, xn, rows, C, w->ln_eps, st) != hipSuccess)
+      return AGG_ERR_LAUNCH;
     const LinearOuts qkv = {{(const uint16_t*)w->w_q, (const uint16_t*)w->w_k, (const uint16_t*)w->w_v},
                             {w->b_q, w->b_k, w->b_v},
                             {(uint16_t*)Q, (uint16_t*)K, (uint16_t*)V},

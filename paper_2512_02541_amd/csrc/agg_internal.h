@@ -144,6 +144,9 @@ hipError_t launch_pool(const Geom& g, const void* K, const void* V, void* Kc, vo
 
 hipError_t launch_layernorm(const void* x, const float* gamma, const float* beta, void* y,
                             int64_t rows, int C, float eps, hipStream_t st);
+// the same, quantised to 4-bit floats in the same pass (codes and scales as launch_mx4_quantize leaves them)
+hipError_t launch_layernorm_mx4(const void* x, const float* gamma, const float* beta, void* codes, void* scales,
+                                int64_t rows, int C, float eps, hipStream_t st);
 // Y_i[rows, N] = A[rows, K] W_i[N, K]^T + bias_i (+ R) for i < count (1..3 weight matrices
 // applied to the same input in one launch); bf16 tensors, float bias (may be null)
 struct LinearOuts {

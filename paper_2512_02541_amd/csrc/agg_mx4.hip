@@ -4,6 +4,7 @@
 
 #include "agg_internal.h"
 #include "agg_lds_copy.h"
+#include "agg_mx4_block.h"
 #include "agg_mx4_plan.h"
 #include "agg_stream.h"
 
@@ -47,20 +48,13 @@ __device__ __forceinline__ f32x4 mfma4(u32x4 a, u32x4 w, f32x4 acc, int sa, int 
   const i32x8 y = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0};
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, acc, 4, 4, kByte, sa, kByte, sw);
 }
-// (by value: a cast of a vector's element itself takes the vector's first)
-__device__ inline bf16x2 as_pair(uint32_t w) { return __builtin_bit_cast(bf16x2, w); }
 __device__ inline float bf16_of(uint32_t bits) { return __uint_as_float(bits << 16); }
 
 }  // namespace
 
 // ---------------------------------------------------------------------------
-// Quantisation: a lane holds eight channels, four lanes a block of 32.  The largest magnitude of a
-// block is the largest of the bf16 patterns without their signs (their order is that of the values,
-// NaN and infinity last), and its exponent field minus 2 is the scale's byte; the conversion
-// instruction divides by the scale and rounds to the nearest, ties to even, saturating.  (For a
-// scale byte of 0 the float with exponent field 0 stands for 2^-127: all 255 scales and all finite bf16
-// values were compared with the definition.)  One wavefront per row; HBM-bound: 137 400 rows of 1024 and back
-// 109 us (712 MB, the codes counted twice), 134 with ordinary accesses to the bf16 tensors.
+// Quantisation: a lane holds eight channels, four lanes a block of 32, one wavefront a row; HBM-bound: 137 400 rows of
+// 1024 and back 109 us (712 MB, the codes counted twice), 134 with ordinary accesses to the bf16 tensors.
 // ---------------------------------------------------------------------------
 constexpr int kQuantThreads = 256;
 
@@ -76,21 +70,8 @@ __global__ __launch_bounds__(kQuantThreads) void mx4_quantize_kernel(
   for (int w = blockIdx.y * 64 + lane; w < words; w += gridDim.y * 64) {
     u32x4 v = {0u, 0u, 0u, 0u};
     if (w < nchunk) v = load16<kStream>(x + row * x_stride + w * 8);
-    uint32_t most = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) most = max(most, max(v[i] & 0x7FFFu, (v[i] >> 16) & 0x7FFFu));
-    most = max(most, (uint32_t)__shfl_xor((int)most, 1));
-    most = max(most, (uint32_t)__shfl_xor((int)most, 2));
-    const uint32_t e = most >> 7;  // 255: NaN or infinity in the block
-    const uint32_t s = e == 255 ? 255u : (e > 2 ? e - 2 : 0u);
-    uint32_t code = 0;
-    if (s != 255) {
-      const float scale = __uint_as_float(s << 23);
-      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, as_pair(v[0]), scale, 0);
-      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, as_pair(v[1]), scale, 1);
-      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, as_pair(v[2]), scale, 2);
-      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, as_pair(v[3]), scale, 3);
-    }
+    uint32_t s;
+    const uint32_t code = mx4_codes(v, s);
     codes[row * words + w] = code;
     if ((w & 3) == 0) scales[row * scale_stride + w / 4] = (uint8_t)s;
   }

@@ -579,6 +579,27 @@ def test_block_chain_hands_its_norm_on():
     assert same_bits(y3, y2) and same_bits(held, n2)
 
 
+@pytest.mark.parametrize("H", [1, 5, 8, 16, 33, 64])
+def test_block_norm_in_four_bits_is_norm_then_four_bits(H):
+    """The block's own norm goes to 4 bits in one pass: the same result as for the norm handed in as a tensor."""
+    say("block norm in four bits", H)
+    shape = agg.make_shape(1, 2, 3, 5, 1, H, 64, 1, 1)
+    C = H * 64
+    wts, x, parts = block_parts(shape, 48)
+    x[0, 3] = 0.0
+    x[0, 4, 7] = float("inf")
+    cw = agg.make_block_weights(*(wts[m] for m in ("ln_gamma", "ln_beta", "ln_eps", "w_q", "w_k", "w_v", "w_o",
+                                                   "b_q", "b_k", "b_v", "b_o")))
+    size = agg.agg_block_workspace_bytes(shape, agg.AGG_BLOCK_FRAME)
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    agg.agg_global_block_fwd(shape, agg.AGG_BLOCK_FRAME, cw, x, torch.empty_like(x), ws, size)
+    xn = ws[:x.numel() * 2].view(torch.bfloat16).view(x.shape).clone()  # a block's workspace begins with its norm
+    want = harness.block_ex_forward(shape, agg.AGG_BLOCK_FRAME, wts, agg.make_block_options(x_norm=xn, **parts), x)
+    got = harness.block_ex_forward(shape, agg.AGG_BLOCK_FRAME, wts, agg.make_block_options(**parts), x)
+    assert torch.isfinite(want[0][0, shape.L:]).all() and torch.isnan(want[0][0, 4]).any()
+    assert same_bits(got[0], want[0]) and same_bits(got[1], want[1])
+
+
 def test_block_without_options_is_the_plain_block():
     say("block plain")
     shape = agg.make_shape(1, 3, 9, 7, 5, 16, 64, 2, 2, 1)
