@@ -522,12 +522,16 @@ template <bool kFourBits>
 static hipError_t launch_norm(const void* x, const float* gamma, const float* beta, void* y, void* scales, int64_t rows,
                               int C, float eps, hipStream_t st) {
   if (C % 8 != 0 || C > 64 * 8 * kLnMaxChunks) return hipErrorInvalidValue;
-  const int64_t groups = (rows + (kLnThreads / 64) - 1) / (kLnThreads / 64);
-  if (groups > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
   (void)hipGetLastError();
   const auto kernel = C <= 64 * 8 * 4 ? layernorm_kernel<4, kFourBits> : layernorm_kernel<kLnMaxChunks, kFourBits>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kLnThreads), 0, st, (const uint16_t*)x, gamma, beta, y, rows, C,
-                     eps, (uint8_t*)scales, (int)(mx4_code_stride(C) / 4), (int)mx4_scale_stride(C));
+  const int words = (int)(mx4_code_stride(C) / 4), scale_stride = (int)mx4_scale_stride(C);
+  const int64_t y_bytes = kFourBits ? words * 4 : C * 2;  // of a row
+  for (int64_t first = 0; first < rows; first += kLaunchRows) {
+    const int64_t here = rows - first < kLaunchRows ? rows - first : kLaunchRows;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((here + kLnThreads / 64 - 1) / (kLnThreads / 64))), dim3(kLnThreads), 0, st,
+                       (const uint16_t*)x + first * C, gamma, beta, (char*)y + first * y_bytes, here, C, eps,
+                       kFourBits ? (uint8_t*)scales + first * scale_stride : nullptr, words, scale_stride);
+  }
   return hipGetLastError();
 }
 

@@ -142,6 +142,10 @@ hipError_t launch_select(const Geom& g, int rule, uint64_t seed, const void* K, 
 hipError_t launch_pool(const Geom& g, const void* K, const void* V, void* Kc, void* Vc,
                        hipStream_t st);
 
+// Rows of a launch that gives each a wavefront.  The threads of a launch are counted with 32 bits along x, and one of
+// 2^32 or more runs what is left of that number modulo 2^32, without an error.
+constexpr int64_t kLaunchRows = (int64_t)1 << 25;
+
 hipError_t launch_layernorm(const void* x, const float* gamma, const float* beta, void* y,
                             int64_t rows, int C, float eps, hipStream_t st);
 // the same, quantised to 4-bit floats in the same pass (codes and scales as launch_mx4_quantize leaves them)

@@ -652,16 +652,13 @@ static dim3 quant_grid(int64_t rows, int words) {
   const int64_t runs = rows < 2048 ? (words + 63) / 64 : 1;
   return dim3((unsigned)((rows + kQuantThreads / 64 - 1) / (kQuantThreads / 64)), (unsigned)(runs < 65535 ? runs : 65535));
 }
-// rows of a launch: its threads are counted with 32 bits
-constexpr int64_t kQuantRows = (int64_t)1 << 25;
-
 hipError_t launch_mx4_quantize(const void* x, int64_t x_stride, void* codes, void* scales, int64_t rows, int K,
                                hipStream_t st) {
   const int words = (int)(mx4_code_stride(K) / 4), scale_stride = (int)mx4_scale_stride(K);
   const auto kernel = streams(rows * K * 2) ? mx4_quantize_kernel<true> : mx4_quantize_kernel<false>;
   (void)hipGetLastError();
-  for (int64_t first = 0; first < rows; first += kQuantRows) {
-    const int64_t here = rows - first < kQuantRows ? rows - first : kQuantRows;
+  for (int64_t first = 0; first < rows; first += kLaunchRows) {
+    const int64_t here = rows - first < kLaunchRows ? rows - first : kLaunchRows;
     hipLaunchKernelGGL(kernel, quant_grid(here, words), dim3(kQuantThreads), 0, st,
                        (const uint16_t*)x + first * x_stride, x_stride, (uint32_t*)codes + first * words,
                        (uint8_t*)scales + first * scale_stride, here, K, words, scale_stride);
@@ -673,8 +670,8 @@ hipError_t launch_mx4_dequantize(const void* codes, const void* scales, void* x,
   const int words = (int)(mx4_code_stride(K) / 4), scale_stride = (int)mx4_scale_stride(K);
   const auto kernel = streams(rows * K * 2) ? mx4_dequantize_kernel<true> : mx4_dequantize_kernel<false>;
   (void)hipGetLastError();
-  for (int64_t first = 0; first < rows; first += kQuantRows) {
-    const int64_t here = rows - first < kQuantRows ? rows - first : kQuantRows;
+  for (int64_t first = 0; first < rows; first += kLaunchRows) {
+    const int64_t here = rows - first < kLaunchRows ? rows - first : kLaunchRows;
     hipLaunchKernelGGL(kernel, quant_grid(here, words), dim3(kQuantThreads), 0, st,
                        (const uint32_t*)codes + first * words, (const uint8_t*)scales + first * scale_stride,
                        (uint16_t*)x + first * K, here, K, words, scale_stride);
