@@ -1202,9 +1202,13 @@ static void launch_both(const AttnArgs& p, dim3 grid, hipStream_t st) {
   }
 }
 
+static int64_t plan_groups(const TilePlan& t, int npairs) {
+  return (int64_t)first_list(t, npairs).groups + second_list(t, npairs).groups;
+}
+
 template <int kSrc>
 static void launch_source(const AttnArgs& p, hipStream_t st) {
-  const dim3 grid((unsigned)(first_list(p.plan, p.npairs).groups + second_list(p.plan, p.npairs).groups));
+  const dim3 grid((unsigned)plan_groups(p.plan, p.npairs));
   const int tail_q = p.plan.n_tail ? p.plan.tail_q : 0;
   if (p.plan.split) hipLaunchKernelGGL(sga_attn_split_kernel<kSrc>, grid, dim3(2 * kAttnThreads), 0, st, p);
   else if (tail_q == 0) launch_both<kSrc, 0>(p, grid, st);
@@ -1217,10 +1221,33 @@ hipError_t launch_attn(const Geom& g, uint32_t flags, float scale, float mean_bi
                        const float* kmean, const float* vmean, void* O, float* lse, hipStream_t st,
                        const uint32_t* kept_bits, const int32_t* nd_dev, int src_mode,
                        const int32_t* list, int64_t list_stride) {
-  const int npairs = g.B * g.H;
+  const int64_t pairs = (int64_t)g.B * g.H;
   // the bound on the grid, with whole pairs per XCD throughout (narrow workgroups: plan_tiles)
-  if ((int64_t)((npairs + kXcds - 1) / kXcds) * kXcds * ((g.NQ + kQTile - 1) / kQTile) > 0x7FFFFFFF)
-    return hipErrorInvalidConfiguration;
+  const bool listed = pairs <= 0x7FFFFFFF - kXcds &&
+                      (pairs + kXcds - 1) / kXcds * kXcds * ((g.NQ + kQTile - 1) / kQTile) <= 0x7FFFFFFF;
+  const int npairs = listed ? (int)pairs : 0;
+  const TilePlan plan = plan_tiles(g.NQ, npairs, g.M_pad / kTileRows);
+  // A launch has fewer than 2^32 threads (kLaunchRows): beyond that each half of the batch is a call of its own.
+  // Per-frame attention, whose frames are the batch here, gets there with 2^24 frames and heads of a few tokens.
+  if (!listed || plan_groups(plan, npairs) > 0xFFFFFFFFll / kAttnThreads) {
+    if (g.B < 2) return hipErrorInvalidConfiguration;
+    Geom half[2] = {g, g};
+    half[0].B = g.B / 2;
+    half[1].B = g.B - half[0].B;
+    int64_t b = 0;
+    for (const Geom& h : half) {
+      const int64_t rows = b * g.NQ * g.H * kHeadDim, kept = b * g.H * g.M_pad * kHeadDim, means = b * g.H * kHeadDim;
+      auto at = [](const void* t, int64_t elements) { return t ? (const uint16_t*)t + elements : nullptr; };
+      const hipError_t e = launch_attn(
+          h, flags, scale, mean_bias, at(Q, rows), at(K, rows), at(V, rows), at(Kc, kept), at(Vc, kept),
+          kmean ? kmean + means : nullptr, vmean ? vmean + means : nullptr, (uint16_t*)O + rows,
+          lse ? lse + b * g.H * g.NQ : nullptr, st, kept_bits ? kept_bits + b * ((g.NQ + 31) / 32) : nullptr,
+          nd_dev ? nd_dev + b : nullptr, src_mode, list ? list + b * list_stride : nullptr, list_stride);
+      if (e != hipSuccess) return e;
+      b += h.B;
+    }
+    return hipSuccess;
+  }
   // indexed rows are addressed with 32-bit byte offsets from the (batch, head) base, formed by
   // a 24-bit multiplication of token id and row length
   if (src_mode == kSrcIndexed && ((uint64_t)g.NQ * g.H * (kHeadDim * 2) > 0xFFFFFFFFull ||
@@ -1242,7 +1269,7 @@ hipError_t launch_attn(const Geom& g, uint32_t flags, float scale, float mean_bi
   p.O = (uint16_t*)O;
   p.lse = lse;
   p.npairs = npairs;
-  p.plan = plan_tiles(g.NQ, npairs, g.M_pad / kTileRows);
+  p.plan = plan;
   p.kept_bits = kept_bits;
   p.nd_dev = nd_dev;
   p.list = list;

@@ -29,3 +29,43 @@ def test_block_of_more_rows_than_a_launch_counts(mx):
         part = y[i:i + 300 * period]
         want = first.repeat(300, 1)[:len(part)]
         assert ops.same_bits(part, want), i
+
+
+def test_frames_of_one_token_beyond_a_launch():
+    """2^24 frames and some, of one token, one head: a key's only query returns its value, and its logit.
+    lse: the kernel multiplies q * scale * log2(e) rounded to bf16, which moves each of the 64 products by up to 2^-8 of
+    its magnitude; their float32 sum and the way to and from base 2 are under 2^-16 of the magnitudes and 1; the weight,
+    rounded to bf16, is off by 2^-8 of itself at most, which is as much in its logarithm."""
+    ops.say("frames of one token")
+    N = (1 << 24) + 9
+    shape = agg.make_shape(1, N, 1, 1, 0, 1, 64, 1, 1)
+    g = ops.gen(50)
+    q, k, v = (torch.randn((1, N, 1, 64), generator=g, device="cuda", dtype=torch.bfloat16) for _ in "qkv")
+    out = harness._buf((1, N, 1, 64), torch.bfloat16, q.device, "O")
+    lse = harness._buf((1, N), torch.float32, q.device, "lse")
+    out.view(torch.int16).fill_(0x7FC1)
+    lse.fill_(float("nan"))
+    agg.agg_frame_attn_fwd(shape, q, k, v, out, lse)
+    assert ops.same_bits(out, v)
+    for at in range(0, N, 1 << 22):
+        part = slice(at, min(N, at + (1 << 22)))
+        both = q[0, part, 0].double() * k[0, part, 0].double() / 8
+        want, size = both.sum(-1), both.abs().sum(-1)
+        assert ((lse[0, part].double() - want).abs() <= 1.01 * 2.0 ** -8 + 2.0 ** -8 * size + 2.0 ** -16 * (size + 1)).all(), at
+
+
+def test_frames_of_some_heads_beyond_a_launch():
+    """The same number of pairs as frames of two tokens and several heads of two sequences: what the parts return."""
+    ops.say("frames of two tokens")
+    B, N, H = 2, 1 << 20, 9
+    shape = agg.make_shape(B, N, 1, 2, 0, H, 64, 1, 1)
+    g = ops.gen(51)
+    q, k, v = (torch.randn((B, 2 * N, H, 64), generator=g, device="cuda", dtype=torch.bfloat16) for _ in "qkv")
+    assert B * N * H > 1 << 24
+    out, _ = harness.frame_forward(shape, q, k, v)
+    part = agg.make_shape(1, 1 << 18, 1, 2, 0, H, 64, 1, 1)
+    for b in range(B):
+        for at in range(0, 2 * N, 1 << 19):
+            rows = slice(at, at + (1 << 19))
+            want, _ = harness.frame_forward(part, q[b:b + 1, rows], k[b:b + 1, rows], v[b:b + 1, rows])
+            assert ops.same_bits(out[b:b + 1, rows], want), (b, at)
