@@ -661,9 +661,9 @@ __device__ inline uint32_t mix32(uint32_t x) {
 
 __global__ __launch_bounds__(256) void select_kernel(Geom g, int rule, uint32_t seed32,
                                                      const uint16_t* __restrict__ K,
-                                                     int32_t* __restrict__ list) {
+                                                     int32_t* __restrict__ list, int64_t first) {
   const int lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t row = first + (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (row >= g.M * g.B) return;  // uniform per wavefront
   const int b = (int)(row / g.M);
   const int64_t m = row % g.M;
@@ -726,12 +726,14 @@ __global__ __launch_bounds__(256) void select_kernel(Geom g, int rule, uint32_t 
 
 hipError_t launch_select(const Geom& g, int rule, uint64_t seed, const void* K, int32_t* list,
                          hipStream_t st) {
-  const int64_t groups = (g.M * g.B + 3) / 4;
-  if (groups > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
+  const int64_t rows = g.M * g.B;
   const uint32_t seed32 = (uint32_t)seed ^ ((uint32_t)(seed >> 32) * 0x9E3779B1u);
   (void)hipGetLastError();
-  hipLaunchKernelGGL(select_kernel, dim3((unsigned)groups), dim3(256), 0, st, g, rule, seed32,
-                     (const uint16_t*)K, list);
+  for (int64_t first = 0; first < rows; first += kLaunchRows) {
+    const int64_t here = rows - first < kLaunchRows ? rows - first : kLaunchRows;
+    hipLaunchKernelGGL(select_kernel, dim3((unsigned)((here + 3) / 4)), dim3(256), 0, st, g, rule, seed32,
+                       (const uint16_t*)K, list, first);
+  }
   return hipGetLastError();
 }
 

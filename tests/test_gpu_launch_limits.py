@@ -69,3 +69,15 @@ def test_frames_of_some_heads_beyond_a_launch():
             rows = slice(at, at + (1 << 19))
             want, _ = harness.frame_forward(part, q[b:b + 1, rows], k[b:b + 1, rows], v[b:b + 1, rows])
             assert ops.same_bits(out[b:b + 1, rows], want), (b, at)
+
+
+def test_selection_beyond_a_launch():
+    """2^26 kept tokens and some, by the grid rule: the host's own list."""
+    ops.say("selection of many")
+    shape = agg.make_shape(1, (1 << 22) + 1, 8, 8, 0, 1, 64, 2, 2, 0)
+    M, _ = agg.agg_kv_count(shape)
+    assert M > 1 << 26
+    got = harness._buf((M,), torch.int32, torch.device("cuda"), "list")
+    got.fill_(-1)
+    agg.agg_select_kv_indices(shape, agg.AGG_SELECT_FIRST, 0, None, got)
+    assert torch.equal(got.cpu(), torch.from_numpy(agg.agg_kv_indices_host(shape)))
