@@ -15,6 +15,7 @@ namespace agg {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kSubThreads = 256;
+constexpr int64_t kMostGroups = 0xFFFFFFFFll / kSubThreads;  // of a launch: fewer than 2^32 threads (kLaunchRows)
 constexpr int kHeadGroup = 4;  // heads repacked per workgroup: 64 rows x 4 heads x 128 B = 32 KiB
 constexpr int kVPad = 72;      // padded row length (elements) of the raw V rows in LDS
 constexpr int kVHead = kTileRows * kVPad + 64;  // elements between two heads' V rows in LDS
@@ -487,7 +488,7 @@ hipError_t launch_subsample(const Geom& g, const void* K, const void* V, void* K
   const int64_t n_gather = want_copy ? (g.M_pad / kTileRows) * nhg : 0;
   const int64_t n_mean = want_mean ? (int64_t)plan.nchunks * plan.ncolblk : 0;
   const int64_t groups = (n_gather + n_mean) * g.B;
-  if (groups > 0x7FFFFFFF || n_gather > 0x3FFFFFFF) return hipErrorInvalidConfiguration;
+  if (groups > kMostGroups || n_gather > 0x3FFFFFFF) return hipErrorInvalidConfiguration;
   (void)hipGetLastError();  // drop any stale error so the check below is this launch's
   if (!want_copy && idx) {
     hipLaunchKernelGGL(index_kernel, dim3((unsigned)((g.M + kSubThreads - 1) / kSubThreads)),
@@ -554,7 +555,7 @@ hipError_t launch_pool(const Geom& g, const void* K, const void* V, void* Kc, vo
   const int nhg = (g.H + kHeadGroup - 1) / kHeadGroup;
   const int64_t n_gather = (g.M_pad / kTileRows) * nhg;
   const int64_t groups = n_gather * g.B;
-  if (groups > 0x7FFFFFFF || n_gather > 0x3FFFFFFF) return hipErrorInvalidConfiguration;
+  if (groups > kMostGroups || n_gather > 0x3FFFFFFF) return hipErrorInvalidConfiguration;
   (void)hipGetLastError();
   hipLaunchKernelGGL(pool_kernel, dim3((unsigned)groups), dim3(kSubThreads), 0, st, g,
                      (const uint16_t*)K, (const uint16_t*)V, (uint16_t*)Kc, (uint16_t*)Vc,
@@ -624,7 +625,7 @@ hipError_t launch_subsample_list(const Geom& g, const int32_t* list, const void*
   const int64_t n_mean = (int64_t)plan.nchunks * plan.ncolblk;
   const int64_t groups = (n_gather + n_mean) * g.B;
   const int64_t set_groups = (g.M * g.B + 255) / 256;
-  if (groups > 0x7FFFFFFF || n_gather > 0x3FFFFFFF || set_groups > 0x7FFFFFFF)
+  if (groups > kMostGroups || n_gather > 0x3FFFFFFF || set_groups > kMostGroups)
     return hipErrorInvalidConfiguration;
   float* partial = (float*)workspace;
   int32_t* cnt = (int32_t*)(partial + (size_t)g.B * plan.nchunks * 2 * g.H * kHeadDim);

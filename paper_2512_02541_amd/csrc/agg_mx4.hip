@@ -387,7 +387,7 @@ static hipError_t launch_mx4_tiles(Mx4LinearArgs p, hipStream_t st) {
   p.gn = (p.N + kTN - 1) / kTN;
   p.by_channels = p.rows < (int64_t)p.N * p.count;  // the operand of more rows is the one that is read once
   const int64_t groups = (p.gm * p.gn * p.count + kGemmXcds - 1) / kGemmXcds * kGemmXcds;
-  if (groups > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
+  if (groups > 0xFFFFFFFFll / (64 * kWM * kWN)) return hipErrorInvalidConfiguration;  // 2^32 threads (kLaunchRows)
   hipLaunchKernelGGL((mx4_tile_kernel<kTM, kTN, kWM, kWN, kStages, kPerSimd>), dim3((unsigned)groups),
                      dim3(64 * kWM * kWN), 0, st, p);
   return hipGetLastError();

@@ -81,3 +81,17 @@ def test_selection_beyond_a_launch():
     got.fill_(-1)
     agg.agg_select_kv_indices(shape, agg.AGG_SELECT_FIRST, 0, None, got)
     assert torch.equal(got.cpu(), torch.from_numpy(agg.agg_kv_indices_host(shape)))
+
+
+def test_means_beyond_a_launch_are_refused():
+    """A workgroup for each of 2^24 sequences and one: an error, and nothing is launched."""
+    ops.say("means of many sequences")
+    B = (1 << 24) + 1
+    shape = agg.make_shape(B, 2, 1, 2, 0, 1, 64, 1, 2, 1)
+    k = torch.empty((B, 4, 1, 64), dtype=torch.bfloat16, device="cuda")
+    means = torch.empty((2, B, 64), dtype=torch.float32, device="cuda")
+    size = agg.agg_workspace_bytes(shape)
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    with pytest.raises(agg.AggError) as e:
+        agg.agg_kv_subsample(shape, k, k, None, None, None, means[0], means[1], ws, size)
+    assert e.value.status == agg.AGG_ERR_LAUNCH
