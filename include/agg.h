@@ -74,7 +74,8 @@ typedef enum agg_status {
   AGG_ERR_UNSUPPORTED = -3, /* D != 64; rows wider than the call takes              */
   AGG_ERR_ALIGN = -4,       /* a tensor pointer is not 16-byte aligned             */
   AGG_ERR_WORKSPACE = -5,   /* workspace smaller than the matching *_workspace_bytes */
-  AGG_ERR_OVERFLOW = -6,    /* N*L, M_pad or a tensor's element count exceeds the index range */
+  AGG_ERR_OVERFLOW = -6,    /* N*L, M_pad, a position, a matrix's rows or channels, or a tensor's element count exceeds
+                               the index range */
   AGG_ERR_LAUNCH = -7       /* hipGetLastError() after a launch was not hipSuccess */
 } agg_status;
 

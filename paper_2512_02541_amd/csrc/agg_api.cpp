@@ -72,11 +72,11 @@ const char* agg_status_string(int status) {
   switch (status) {
     case AGG_OK: return "ok";
     case AGG_ERR_NULL: return "a required pointer is NULL";
-    case AGG_ERR_SHAPE: return "invalid shape, stride, scale or flag";
-    case AGG_ERR_UNSUPPORTED: return "unsupported head dimension (D must be 64)";
+    case AGG_ERR_SHAPE: return "invalid shape, stride, scale or flag, or buffers overlap that may not";
+    case AGG_ERR_UNSUPPORTED: return "head dimension is not 64, or rows are wider than the call takes";
     case AGG_ERR_ALIGN: return "tensor pointer is not 16-byte aligned";
     case AGG_ERR_WORKSPACE: return "workspace too small";
-    case AGG_ERR_OVERFLOW: return "sequence too long for 32-bit token ids";
+    case AGG_ERR_OVERFLOW: return "a size or a position exceeds the index range";
     case AGG_ERR_LAUNCH: return "kernel launch failed";
     default: return "unknown status";
   }

@@ -277,3 +277,22 @@ def test_block_refusals():
     lib = agg.lib()
     assert lib.agg_global_block_ex_fwd(ctypes.byref(shape), 0, ctypes.byref(weights), None, _at(0), _at(1), None,
                                        _at(2), 1 << 40, None) == N
+
+
+def test_errors_say_what_the_operators_refuse():
+    """A status that several calls share names the reasons of all of them."""
+    def message(call):
+        with pytest.raises(agg.AggError) as e:
+            call()
+        return str(e.value)
+
+    r, m = agg.make_residual(), agg.make_mx4_linear([(_at(2), _at(3))], [_at(9)])
+    wide = message(lambda: agg.agg_residual_norm_fwd(1, 8200, r, _at(0), _at(1), _at(2), None, stream=0))
+    assert "wider" in wide and "head dimension" in wide
+    over = message(lambda: agg.agg_residual_norm_fwd(4, 64, r, _at(0), _at(1), _at(0) + 64, None, stream=0))
+    assert "overlap" in over and "shape" in over
+    deep = message(lambda: agg.agg_mx4_linear_fwd(1, 64, 1 << 23, m, _at(0), _at(1), stream=0))
+    far = message(lambda: agg.agg_rope_fwd(agg.make_shape(1, 2, 16, 16, 5, 16, 64, 1, 1),
+                                           agg.make_rope(agg.AGG_ROPE_HEAD, 16, 24, 24, t0=2 ** 31 - 2), None, None, None,
+                                           _at(0), 0, None, 0, _at(2), None, stream=0))
+    assert deep.split(": ")[1] == far.split(": ")[1] and "size" in deep and "position" in far and "token" not in deep
