@@ -333,8 +333,8 @@ typedef struct agg_rope {
  * rotation.  Q, K: device bf16, token t of batch element b at element (b*N*L + t) * stride, stride 0
  * meaning H*D (contiguous), otherwise a multiple of 8 and >= H*D: a fused projection's output is read
  * where it is.  Qr, Kr: [B, N*L, H, D], contiguous.  Qr = Q and Kr = K (contiguous) work in place;
- * other overlaps of an output with an input or the other output are refused with AGG_ERR_SHAPE.  Q and Qr may both be
- * NULL, or K and Kr.  Of `shape` only B, N, n_h, n_w, n_special, H and D matter.
+ * other overlaps of an output with an input, its norms' parameters, `pos` or the other output are refused with
+ * AGG_ERR_SHAPE.  Q and Qr may both be NULL, or K and Kr.  Of `shape` only B, N, n_h, n_w, n_special, H and D matter.
  */
 int agg_rope_fwd(const agg_shape* shape, const agg_rope* rope, const agg_norm* q_norm,
                  const agg_norm* k_norm, const int32_t* pos, const void* Q, int64_t q_stride,
@@ -347,8 +347,8 @@ int agg_rope_fwd(const agg_shape* shape, const agg_rope* rope, const agg_norm* q
  * x, branch, h, n: device bf16 [rows, C].  scale: device float32 [C], 16-byte aligned (NULL: ones).  gate: device bf16
  * [ceil(rows / gate_rows), C], row r uses gate[r / gate_rows] (NULL: ones; gate_rows is then
  * ignored).  branch NULL: h = x.  h may be NULL (not written); n must be given exactly if pre.kind
- * is not NONE.  h = x, h = branch, n = x and n = branch work in place; other overlaps of outputs with x, branch, gate or each
- * other are refused with AGG_ERR_SHAPE.  C: a multiple of 8, at most 8192 (AGG_ERR_UNSUPPORTED).  rows = 0: nothing is done.
+ * is not NONE.  h = x, h = branch, n = x and n = branch work in place; other overlaps of outputs with x, branch, gate, scale,
+ * the norms' parameters or each other are refused with AGG_ERR_SHAPE.  C: a multiple of 8, at most 8192 (AGG_ERR_UNSUPPORTED).  rows = 0: nothing is done.
  */
 typedef struct agg_residual {
   agg_norm post, pre;
@@ -391,7 +391,8 @@ int agg_mx4_dequantize(int64_t rows, int32_t K, const void* codes, const void* s
  *     Y = R + res_scale * (A W^T + bias)
  * A: [rows, K] and W_i: [N, K] in 4 bits; products and sums in float32, one rounding.  bias_i: float32
  * [N], 16-byte aligned, or NULL.  Y_i, R: bf16 [rows, N], contiguous; Y = R works in place, other
- * overlaps of an output with R, A, a W_i or another output are refused with AGG_ERR_SHAPE.  res_scale: like bias_i (NULL: ones; must be NULL without R).
+ * overlaps of an output with R, A, a W_i, a bias, res_scale or another output are refused with AGG_ERR_SHAPE.  res_scale:
+ * like bias_i (NULL: ones; must be NULL without R).
  * K and N are multiples of 8, K at most 2^22 and N at most 2^21.  rows = 0: nothing is done.  The order of a row's sums
  * depends on the call's sizes and the row's place in it, not on the other rows.
  */

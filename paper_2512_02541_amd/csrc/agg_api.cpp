@@ -361,6 +361,11 @@ bool overlap(const void* a, uint64_t na, const void* b, uint64_t nb) {
   return x < y ? y - x < na : x - y < nb;
 }
 
+// whether an output shares a byte with the parameters of a norm over C channels
+bool overlap_norm(const void* out, uint64_t bytes, const SeamNorm& n, int64_t C) {
+  return overlap(out, bytes, n.gamma, (uint64_t)C * 4) || overlap(out, bytes, n.beta, (uint64_t)C * 4);
+}
+
 int make_norm(const agg_norm* n, SeamNorm* out) {
   *out = SeamNorm{AGG_NORM_NONE, 1.f, nullptr, nullptr};
   if (!n || n->kind == AGG_NORM_NONE) return AGG_OK;
@@ -459,6 +464,8 @@ int make_rope_args(const agg_shape* shape, const agg_rope* rope, const agg_norm*
     if (!in_place && overlap(in[t], in_bytes[t], out[t], out_bytes)) return AGG_ERR_SHAPE;
     if (overlap(in[1 - t], in_bytes[1 - t], out[t], out_bytes)) return AGG_ERR_SHAPE;
     if (pos && overlap(pos, (uint64_t)a->total * 12, out[t], out_bytes)) return AGG_ERR_SHAPE;
+    for (const SeamNorm& n : a->norm)
+      if (overlap_norm(out[t], out_bytes, n, kHeadDim)) return AGG_ERR_SHAPE;
   }
   if (overlap(Qr, out_bytes, Kr, out_bytes)) return AGG_ERR_SHAPE;
   a->pos = pos;
@@ -494,7 +501,9 @@ int make_seam_args(int64_t rows, int32_t C, const agg_residual* r, const void* x
   for (void* o : out) {
     if (o != x && overlap(o, bytes, x, bytes)) return AGG_ERR_SHAPE;
     if (o != branch && overlap(o, bytes, branch, bytes)) return AGG_ERR_SHAPE;
-    if (overlap(o, bytes, r->gate, (uint64_t)groups * C * 2)) return AGG_ERR_SHAPE;
+    if (overlap(o, bytes, r->gate, (uint64_t)groups * C * 2) || overlap(o, bytes, r->scale, (uint64_t)C * 4) ||
+        overlap_norm(o, bytes, a->post, C) || overlap_norm(o, bytes, a->pre, C))
+      return AGG_ERR_SHAPE;
   }
   if (overlap(h, bytes, n, bytes)) return AGG_ERR_SHAPE;
   a->x = (const uint16_t*)x;
@@ -543,13 +552,15 @@ int make_mx4_args(int64_t rows, int32_t N, int32_t K, const agg_mx4_linear* l, c
       if (overlap(l->y[i], y_bytes, l->y[j], y_bytes)) return AGG_ERR_SHAPE;
     for (int j = 0; j < l->count; ++j)
       if (overlap(l->y[i], y_bytes, l->w[j].codes, (uint64_t)N * mx4_code_stride(K)) ||
-          overlap(l->y[i], y_bytes, l->w[j].scales, (uint64_t)N * mx4_scale_stride(K)))
+          overlap(l->y[i], y_bytes, l->w[j].scales, (uint64_t)N * mx4_scale_stride(K)) ||
+          overlap(l->y[i], y_bytes, l->bias[j], (uint64_t)N * 4))
         return AGG_ERR_SHAPE;
     a->w[i] = Mx4Matrix{(const uint8_t*)l->w[i].codes, (const uint8_t*)l->w[i].scales};
     a->bias[i] = l->bias[i];
     a->y[i] = (uint16_t*)l->y[i];
   }
   if (l->residual != l->y[0] && overlap(l->residual, y_bytes, l->y[0], y_bytes)) return AGG_ERR_SHAPE;
+  if (overlap(l->y[0], y_bytes, l->res_scale, (uint64_t)N * 4)) return AGG_ERR_SHAPE;
   a->a = Mx4Matrix{(const uint8_t*)codes, (const uint8_t*)scales};
   a->residual = (const uint16_t*)l->residual;
   a->res_scale = l->res_scale;

@@ -296,3 +296,31 @@ def test_errors_say_what_the_operators_refuse():
                                            agg.make_rope(agg.AGG_ROPE_HEAD, 16, 24, 24, t0=2 ** 31 - 2), None, None, None,
                                            _at(0), 0, None, 0, _at(2), None, stream=0))
     assert deep.split(": ")[1] == far.split(": ")[1] and "size" in deep and "position" in far and "token" not in deep
+
+
+def test_outputs_over_parameters_are_refused():
+    """Parameters are read while outputs are written: an overlap would let rows already written change the others."""
+    S = agg.AGG_ERR_SHAPE
+    rows = 522 * 2048
+    for at, out in ((2, "qr"), (3, "kr")):
+        for near in (_at(at), _at(at) + rows - 16, _at(at) - 240):
+            for n in (agg.make_norm(agg.AGG_NORM_LAYER, 1e-5, near), agg.make_norm(agg.AGG_NORM_RMS, 1e-5, None, near)):
+                assert _rope(q_norm=n) == S and _rope(k_norm=n) == S, out
+    for at in (2, 3):  # h, n
+        for near in (_at(at), _at(at) + 10 * 2048 - 16, _at(at) - 4080):
+            assert _seam(scale=near) == S
+            for n in (agg.make_norm(agg.AGG_NORM_LAYER, 1e-5, near), agg.make_norm(agg.AGG_NORM_RMS, 1e-5, None, near)):
+                assert _seam(post=n) == S
+                r = agg.make_residual(pre=n)
+                assert _status(agg.agg_residual_norm_fwd, 10, 1024, r, _at(0), _at(1), _at(2), _at(3)) == S
+    for near in (_at(10), _at(10) + 10 * 2048 - 16, _at(10) - 4080):
+        assert _linear(biases=[near]) == S and _linear(count=2, biases=[None, near]) == S
+        assert _linear(residual=_at(5), res_scale=near) == S
+    # the y of a block is its residual norm's, or its output projection's
+    shape = agg.make_shape(1, 2, 16, 16, 5, 16, 64, 2, 2)
+    w = agg.agg_block_weights(_at(20), _at(21), 1e-6, _at(22), _at(23), _at(24), _at(25), None, None, None, _at(1) + 64)
+    mx = [(_at(30 + 2 * i), _at(31 + 2 * i)) for i in range(4)]
+    scaled = agg.make_residual(scale=_at(1) + 1024)
+    for o, weights in ((agg.make_block_options(mx=mx), w), (agg.make_block_options(residual=scaled), w)):
+        assert _status(agg.agg_global_block_ex_fwd, shape, agg.AGG_BLOCK_FRAME, weights, o, _at(0), _at(1), None, _at(2),
+                       1 << 40) == S
