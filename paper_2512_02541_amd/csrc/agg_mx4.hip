@@ -108,8 +108,9 @@ __global__ __launch_bounds__(kQuantThreads) void mx4_dequantize_kernel(
 //
 // For few rows: 16 tokens x 16 channels a workgroup, whose eight wavefronts share k; their sums meet
 // in LDS, in a fixed order.  What counts is one chain of latencies: fragments come straight from memory,
-// up to four steps of 128 channels under way at once.  Measured: 1 row of 1024 -> 1024 2.7 us, of 4096 -> 1024 4.1
-// (7.2 and 15.7 in a 32 x 64 tile a wavefront); 64 rows of 4096 -> 1024 5.8.
+// up to four steps of 128 channels under way at once.  Measured, each of many in a graph: 1 row of 1024 -> 1024 2.7 to
+// 3.1 us (3.3 to 3.6 alone), of 4096 -> 1024 4.1 to 4.4 (7.2 and 15.7 in a 32 x 64 tile a wavefront); 64 rows of
+// 4096 -> 1024 5.8 to 6.1.
 // ---------------------------------------------------------------------------
 constexpr int kFewWaves = 8;
 
@@ -182,7 +183,10 @@ __global__ __launch_bounds__(64 * kFewWaves) void mx4_few_kernel(Mx4LinearArgs p
 // With one stage nothing hides inside a workgroup: four of them share a CU, and one's copies and stores run beside
 // another's products; with fewer tiles two stages are faster (the plan has both sides).  Outputs are stored past
 // the caches, whose lines the operands need: Q/K/V of 137 400 x 1024 in tiles of 128, four on a CU,
-// 451 us through them, 326 past them.
+// 451 us through them, 326 past them.  For few rows it makes no difference: blocks of 1 to 16 frames, whose attention
+// reads Q, K and V at once, the same within 1 %.
+// Some hundred rows are a chain of copies with one step under way: Q/K/V of 522 x 1024 5.6 us (6.3 alone) where their
+// bytes take 1.1, 1374 x 4096 -> 1024 10.1 against 1.8, 2748 rows 14.1 against 3.5.
 // Measured: 21 984 x 4096 -> 1024 60 us without a residual, 64 with one (184 GFLOP: 3.1 PFLOP/s); 21 984 x 4096 -> 4096
 // 197 us (3.7 PFLOP/s, tiles of 256; MFMAs alone on random codes reach 6.3 to 6.8, limited by power: 9.6 on zeros).  A step of
 // a 256-wide tile takes 1.5 us, of which its products are 0.9; its copies alone and its products with their fragment
@@ -405,7 +409,7 @@ static hipError_t launch_mx4_tiles(Mx4LinearArgs p, hipStream_t st) {
 // Measured: Q/K/V of 137 400 x 1024 (864 GFLOP, 844 MB of outputs) 232 us, 3.7 PFLOP/s; 250 with all wavefronts
 // storing at a pass's end, 315 in tiles.  Without its stores 186, without its products 192, products and fragment
 // reads alone 173: products (power) and stores (a kernel that does nothing else writes this pattern in 165 us) bound it
-// together.  K = 512, 3 x 512 channels: 93 us against 113.  With a residual, read like the stores are written and two
+// together.  With few passes a workgroup its start and end count: 21 984 rows 52 us, 12 of them outside the nine passes.  K = 512, 3 x 512 channels: 93 us against 113.  With a residual, read like the stores are written and two
 // 16-token tiles a wavefront for the registers, it was no faster than tiles (163 to 181 us against 173).
 // ---------------------------------------------------------------------------
 constexpr int kPanelThreads = 512;

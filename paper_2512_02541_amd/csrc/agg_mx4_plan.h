@@ -36,7 +36,9 @@ static inline int64_t mx4_passes(int64_t rows, int64_t N, int count) {
   return (rows + kPanelRows - 1) / kPanelRows * ((N + kPassChannels - 1) / kPassChannels) * count;
 }
 
-// Measured in us, each side of a border by both kernels (N, K, matrices: rows: this side / the other):
+// Measured in us, each side of a border by both kernels (N, K, matrices: rows: this side / the other).  The first border
+// was measured with 32 rows and more; of few rows it sends wide or deep products to tiles that walk all of k in
+// one workgroup: 1 row 11008 -> 4096 12.8 us, where its weights' bytes take 4.9.
 //   few        1024, 1024, 3: 32: 4.1 / 4.6 with tiles of 64, 64: 5.0 / 4.6; 1024, 1024, 1: 128: 4.2 / 4.6,
 //              261: 7.3 / 4.6; 1024, 4096, 1: 64: 5.8 / 7.8, 128: 9.3 / 8.0
 //   tiles 64   1024, 1024, 3: 1044: 7.4 / 8.2 with 128, 1374: 9.5 / 9.4; 1024, 4096, 1: 2748: 14.4 / 15.2,
@@ -53,7 +55,7 @@ static inline Mx4Plan plan_mx4(int64_t rows, int64_t N, int64_t K, int count, bo
   if (mx4_tiles(rows, N, count, 64) <= 4 * kGemmCus) return {0, kMx4Tile64};
   if (K <= kPanelMostK && !residual && mx4_passes(rows, N, count) >= 8 * kGemmCus) return {0, kMx4Panel};
   if (K > kPanelMostK) {
-    // whole rounds of large tiles; a last round that is more than half full counts as one
+    // whole rounds of large tiles; a last round that is more than six tenths full counts as one
     const int64_t per_m = (N + 255) / 256 * count, tiles = mx4_tiles(rows, N, count, 256);
     const int64_t rounds = tiles / kGemmCus;
     if (tiles - rounds * kGemmCus > kGemmCus * 6 / 10 || tiles == rounds * kGemmCus) return {0, kMx4Tile256};

@@ -6,6 +6,8 @@
 // finds its input in the caches: with the norm of 21 984 rows stored past them a block in bf16 takes 360 us instead
 // of 351, and loads past them are slower from there (5496 rows: 13.3 instead of 11.7 us).  What is read again only much later (the
 // residual sum, until the next seam) is always stored past them: 21 984 rows 36.6 -> 35.1 us, blocks the same or 1 % faster.
+// So are, by their own measurements, the rotary calls' queries and keys and the 4-bit products' results (rope_kernel,
+// mx4_tile_kernel).
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -75,10 +75,17 @@ __device__ inline void wave_lds_fence() {
 // passed to all heads through LDS.  The angle of a pair in turns is position * frequency
 // modulo 1: a 64-bit product of the position and the frequency in units of 2^-64 turns wraps to
 // exactly that.  A pair's other channel comes out of LDS too, which serves every pairing alike.
-// Bound by HBM once enough is under way: a round's rows are requested while the one before is worked on.
+// Bound by HBM once enough is under way: a round's rows are requested before the one in hand is worked on, and awaited at
+// its end together with its stores (the accesses are conditional, so the compiler counts none of them apart); four
+// wavefronts on a SIMD cover that.
 // Measured (16 frames of 16 heads with a LayerNorm, 180 MB / 100 frames with RMS and given positions, 1.13 GB): 49 / 323 us
 // when rows were requested in their own round and sums went through LDS; 38 / 223 without that; 34 / 207 (5.4 TB/s) with a
-// table of cosine and signed sine per channel, whose reads stand in front of their uses.  One frame of 261 tokens of 8 heads 4 us.
+// table of cosine and signed sine per channel, whose reads stand in front of their uses.  One frame of 261 tokens of 8 heads
+// 4.1 us each of many in a graph, 5.1 to 5.4 alone; a copy in this form takes 2.9: the parameters' loads, the rows' and
+// the positions' wait for each other in front of the first round.
+// Outputs are stored past the caches at every size: 2 frames of 16 heads 7.9 us, 8.9 through them, 100 frames 210 and 217;
+// with the per-frame attention behind it 33.0 and 34.6 (1 frame of 8 heads 12.0 and 11.6, 8 frames 82 and 80), blocks of
+// 1 to 16 frames the same within 1 %.
 // ---------------------------------------------------------------------------
 constexpr int kRopeThreads = 256;
 constexpr int kRopeWaves = kRopeThreads / 64;
@@ -254,10 +261,12 @@ hipError_t launch_rope(const RopeArgs& args, hipStream_t st) {
 // ---------------------------------------------------------------------------
 // h = x + gate * scale * post(branch),  n = pre(h).  A row is in registers in float32, statistics as in
 // layernorm_kernel (mean, then variance of the centred values); norms' parameters stay in registers
-// from row to row, and the next row is requested before the present one is worked on.
+// from row to row, and the next row is requested before the present one is worked on (and awaited behind that one's stores,
+// as in rope_kernel).
 // Rows of up to 1024 channels: one wavefront each, kPer 16-byte chunks a lane.  Few longer ones: the
 // whole workgroup, of as many wavefronts as the row fills, whose sums meet in LDS.
-// HBM-bound: 21 984 rows of 1024 with layer scale and LayerNorm 28 to 29 us (180 MB), 137 400 rows 200 (5.6 TB/s); one row 2.4 us.
+// HBM-bound: 21 984 rows of 1024 with layer scale and LayerNorm 28 to 29 us (180 MB, much of it in the cache where a loop
+// repeats the call; 35 on other tensors each time), 137 400 rows 200 (5.6 TB/s); one row 2.5 us alone, 3.3 each of many in a graph.
 // ---------------------------------------------------------------------------
 namespace {
 
