@@ -1223,13 +1223,14 @@ hipError_t launch_attn(const Geom& g, uint32_t flags, float scale, float mean_bi
                        const int32_t* list, int64_t list_stride) {
   const int64_t pairs = (int64_t)g.B * g.H;
   // the bound on the grid, with whole pairs per XCD throughout (narrow workgroups: plan_tiles)
-  const bool listed = pairs <= 0x7FFFFFFF - kXcds &&
-                      (pairs + kXcds - 1) / kXcds * kXcds * ((g.NQ + kQTile - 1) / kQTile) <= 0x7FFFFFFF;
-  const int npairs = listed ? (int)pairs : 0;
+  if (pairs > 0x7FFFFFFF - kXcds ||
+      (pairs + kXcds - 1) / kXcds * kXcds * ((g.NQ + kQTile - 1) / kQTile) > 0x7FFFFFFF)
+    return hipErrorInvalidConfiguration;
+  const int npairs = (int)pairs;
   const TilePlan plan = plan_tiles(g.NQ, npairs, g.M_pad / kTileRows);
   // A launch has fewer than 2^32 threads (kLaunchRows): beyond that each half of the batch is a call of its own.
   // Per-frame attention, whose frames are the batch here, gets there with 2^24 frames and heads of a few tokens.
-  if (!listed || plan_groups(plan, npairs) > 0xFFFFFFFFll / kAttnThreads) {
+  if (plan_groups(plan, npairs) > 0xFFFFFFFFll / kAttnThreads) {
     if (g.B < 2) return hipErrorInvalidConfiguration;
     Geom half[2] = {g, g};
     half[0].B = g.B / 2;

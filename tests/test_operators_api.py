@@ -324,3 +324,10 @@ def test_outputs_over_parameters_are_refused():
     for o, weights in ((agg.make_block_options(mx=mx), w), (agg.make_block_options(residual=scaled), w)):
         assert _status(agg.agg_global_block_ex_fwd, shape, agg.AGG_BLOCK_FRAME, weights, o, _at(0), _at(1), None, _at(2),
                        1 << 40) == S
+
+
+def test_more_pairs_than_a_launch_plan_counts_are_refused():
+    """2^34 and 2^33 + 2^5 (frame, head) pairs: numbers whose last 32 bits are 0 and 32."""
+    for N in (1 << 30, (1 << 29) + 2):
+        shape = agg.make_shape(1, N, 1, 1, 0, 16, 64, 1, 1)
+        assert _status(agg.agg_frame_attn_fwd, shape, _at(0), _at(1), _at(2), _at(3), None) == agg.AGG_ERR_LAUNCH
