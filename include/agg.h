@@ -440,6 +440,76 @@ int agg_global_block_ex_fwd(const agg_shape* shape, int mode, const agg_block_we
                             const agg_block_options* options, const void* x, void* y, void* n,
                             void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/*
+ * ---- Keys and values of another set, and a paged cache of them ----
+ * Attention of queries to keys and values of another length: of a few tokens (a pose token, tracked points) to a frame's, of
+ * a frame to the frames before it.  For every query i < q_lens[b] of batch element b and every head h
+ *     O[b, i, h] = softmax over j < k_lens[b] of scale*<Q[b, i, h], K[b, j, h']>,  times V[b, j, h'],   h' = h / (H / H_kv).
+ * A batch element without keys has O = 0 and lse = -infinity.  Keys and values at k_lens[b] and behind it are not
+ * looked at, whatever they hold; rows of O and lse at q_lens[b] and behind it are left as they were.
+ */
+typedef struct agg_cross {
+  int32_t B;             /* batch elements                                                           */
+  int32_t NQ, NK;        /* most queries and most keys of one; 0: none                               */
+  int32_t H, H_kv, D;    /* heads of Q and O; of K and V, which divides H; 64                        */
+  float scale;           /* softmax scale                                                            */
+  const int32_t* q_lens; /* device int32 [B], clamped to 0 .. NQ; NULL: NQ                           */
+  const int32_t* k_lens; /* device int32 [B], clamped to 0 .. NK; NULL: NK                           */
+} agg_cross;
+
+/* Host only.  Scratch bytes that the two attention calls below need for these sizes (0: none, the pointer may be NULL; 0 too on
+ * invalid sizes).  Calls that may overlap in time need a workspace each, as do graphs that are replayed side by side. */
+size_t agg_cross_workspace_bytes(const agg_cross* cross);
+
+/*
+ * Keys and values where they are: token t of batch element b at element (b*NK + t) * stride of K and of V (queries: (b*NQ + t) *
+ * stride of Q), stride 0 meaning contiguous, otherwise a multiple of 8 and at least heads * 64.  Q, K, V: device bf16.
+ * O: device bf16 [B, NQ, H, 64], contiguous; lse: device float32 [B, H, NQ] or NULL.  O and lse may overlap nothing else of
+ * the call (AGG_ERR_SHAPE).  The logits of calls with more than 64 queries a key head are those of agg_dense_global_attn_fwd,
+ * with scale*log2(e)*Q rounded to bf16; with fewer they are float32 throughout.
+ */
+int agg_cross_attn_fwd(const agg_cross* cross, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
+                       const void* V, int64_t v_stride, void* O, float* lse, void* workspace,
+                       size_t workspace_bytes, void* hip_stream);
+
+/*
+ * A cache of keys and values in pages of 64 rows, for frames that arrive one after another.  A pool holds n_pages * H * 4096 bf16
+ * (agg_cache_bytes): page p of head h is one 64-row tile in fragment order (above) at element (p*H + h) * 4096.  Row r of sequence
+ * b lies in page pages[b, r / 64], row r % 64 of the tile.  The caller hands pages out; sequences may share pages they only
+ * read, for instance the frames of a clip, each a sequence of its own length over one row of the table (attention that is
+ * causal by frames).  A page number outside the pool is never written, and read as page 0 or the last one.
+ */
+typedef struct agg_cache {
+  int32_t n_pages;        /* pages of a pool                            */
+  int32_t H, D;           /* heads of keys and values; 64               */
+  int32_t B, max_pages;   /* sequences, and entries of each in `pages`  */
+  void *Kc, *Vc;          /* the pools, device bf16, 16-byte aligned    */
+  const int32_t* pages;   /* device int32 [B, max_pages]                */
+} agg_cache;
+
+/* Host only.  Bytes of ONE pool. */
+int agg_cache_bytes(const agg_cache* cache, size_t* bytes);
+
+/*
+ * Appends N*L new tokens per sequence, of which the first counts[b] exist (NULL: all): token t of sequence b becomes row start[b] + t
+ * of the cache (start NULL: row t).  Keys pass through k_norm and the rotation on the way, and queries, if given, through
+ * q_norm and the rotation to Qr, exactly as in agg_rope_fwd, whose conventions (norms, positions by `pos` or by the token's place,
+ * strides, Qr = Q in place) hold here; values go as they are.  shape: B, N, n_h, n_w, n_special as there, H the heads of Q, a multiple
+ * of cache->H (without Q it does not matter).  Rows before 0 and from 64*max_pages on are not stored.  lens (device int32 [B], may be
+ * NULL) receives start[b] + counts[b], clamped to 0 .. 64*max_pages: what k_lens of the next call is.  Everything else in the
+ * pools, and Qr of tokens that do not exist, is left as it was.  Two tokens of one call may not share a row.  No output may overlap
+ * another operand of the call (AGG_ERR_SHAPE); lens may not be start.
+ */
+int agg_cache_append(const agg_cache* cache, const agg_shape* shape, const agg_rope* rope, const agg_norm* q_norm,
+                     const agg_norm* k_norm, const int32_t* pos, const void* Q, int64_t q_stride, const void* K,
+                     int64_t k_stride, const void* V, int64_t v_stride, const int32_t* start, const int32_t* counts,
+                     int32_t* lens, void* Qr, void* hip_stream);
+
+/* agg_cross_attn_fwd over a cache: keys and values of batch element b are the first k_lens[b] rows of its sequence.  cross: B and
+ * H_kv are the cache's B and H, NK at most 64*max_pages. */
+int agg_cache_attn_fwd(const agg_cache* cache, const agg_cross* cross, const void* Q, int64_t q_stride, void* O,
+                       float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

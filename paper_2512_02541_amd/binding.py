@@ -71,6 +71,8 @@ EXPORTS = [
     "agg_rope_fwd", "agg_residual_norm_fwd",
     "agg_mx4_code_stride", "agg_mx4_scale_stride", "agg_mx4_quantize", "agg_mx4_dequantize",
     "agg_mx4_linear_fwd", "agg_block_ex_workspace_bytes", "agg_global_block_ex_fwd",
+    "agg_cross_workspace_bytes", "agg_cross_attn_fwd",
+    "agg_cache_bytes", "agg_cache_append", "agg_cache_attn_fwd",
 ]
 
 AGG_SELECT_FIRST = 0
@@ -142,6 +144,18 @@ class agg_block_options(ctypes.Structure):
                 ("x_norm", ctypes.c_void_p), ("mx", ctypes.POINTER(agg_mx4_matrix))]
 
 
+class agg_cross(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("NQ", ctypes.c_int32), ("NK", ctypes.c_int32),
+                ("H", ctypes.c_int32), ("H_kv", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("q_lens", ctypes.c_void_p), ("k_lens", ctypes.c_void_p)]
+
+
+class agg_cache(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int32), ("H", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("B", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("Kc", ctypes.c_void_p),
+                ("Vc", ctypes.c_void_p), ("pages", ctypes.c_void_p)]
+
+
 # The structs below hold on to the tensors whose addresses they carry.
 def make_norm(kind=AGG_NORM_NONE, eps=1e-5, gamma=None, beta=None) -> agg_norm:
     n = agg_norm(int(kind), float(eps), _ptr(gamma), _ptr(beta))
@@ -197,6 +211,23 @@ def make_block_options(rope=None, pos=None, q_norm=None, k_norm=None, residual=N
         held = None
     o.keep = (rope, pos, q_norm, k_norm, residual, x_norm, mx, held)
     return o
+
+
+def make_cross(B, NQ, NK, H, H_kv=None, D=64, scale=None, q_lens=None, k_lens=None) -> agg_cross:
+    """H_kv None: as many key heads as query heads."""
+    c = agg_cross(int(B), int(NQ), int(NK), int(H), int(H if H_kv is None else H_kv), int(D),
+                  float(1.0 / (D ** 0.5) if scale is None else scale), _ptr(q_lens), _ptr(k_lens))
+    c.keep = (q_lens, k_lens)
+    return c
+
+
+def make_cache(Kc, Vc, pages, H, D=64, n_pages=None) -> agg_cache:
+    """pages: int32 [sequences, pages of each] on the device.  n_pages None: as many as the tensor Kc holds."""
+    B, max_pages = (int(n) for n in pages.shape)
+    c = agg_cache(int(Kc.numel() // (H * 64 * 64) if n_pages is None else n_pages), int(H), int(D), B, max_pages,
+                  _ptr(Kc), _ptr(Vc), _ptr(pages))
+    c.keep = (Kc, Vc, pages)
+    return c
 
 
 def lib():
@@ -263,6 +294,14 @@ def lib():
     L.agg_block_ex_workspace_bytes.argtypes = [shp, ctypes.c_int, opts]
     L.agg_global_block_ex_fwd.argtypes = [shp, ctypes.c_int, ctypes.POINTER(agg_block_weights), opts, vp, vp, vp,
                                           vp, ctypes.c_size_t, vp]
+    crs, cch = ctypes.POINTER(agg_cross), ctypes.POINTER(agg_cache)
+    L.agg_cross_workspace_bytes.restype = ctypes.c_size_t
+    L.agg_cross_workspace_bytes.argtypes = [crs]
+    L.agg_cross_attn_fwd.argtypes = [crs, vp, i64, vp, i64, vp, i64, vp, vp, vp, ctypes.c_size_t, vp]
+    L.agg_cache_bytes.argtypes = [cch, ctypes.POINTER(ctypes.c_size_t)]
+    L.agg_cache_append.argtypes = [cch, shp, ctypes.POINTER(agg_rope), normp, normp, vp, vp, i64, vp, i64, vp, i64,
+                                   vp, vp, vp, vp, vp]
+    L.agg_cache_attn_fwd.argtypes = [cch, crs, vp, i64, vp, vp, vp, ctypes.c_size_t, vp]
     global _raw_stream, _initialized, _device
     # the current stream's handle without building a Stream object for it (3 us a call)
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -488,3 +527,34 @@ def agg_global_block_ex_fwd(shape, mode, weights, options, x, y, n, workspace, w
     _check(lib().agg_global_block_ex_fwd(ctypes.byref(shape), int(mode), ctypes.byref(weights),
                                          ctypes.byref(options), _ptr(x), _ptr(y), _ptr(n), _ptr(workspace),
                                          int(workspace_bytes), _stream(stream)), "agg_global_block_ex_fwd")
+
+
+def agg_cross_workspace_bytes(cross: agg_cross) -> int:
+    return int(lib().agg_cross_workspace_bytes(ctypes.byref(cross)))
+
+
+def agg_cross_attn_fwd(cross, Q, q_stride, K, k_stride, V, v_stride, O, lse=None, workspace=None, workspace_bytes=0,
+                       stream=None):
+    _check(lib().agg_cross_attn_fwd(ctypes.byref(cross), _ptr(Q), int(q_stride), _ptr(K), int(k_stride), _ptr(V),
+                                    int(v_stride), _ptr(O), _ptr(lse), _ptr(workspace), int(workspace_bytes),
+                                    _stream(stream)), "agg_cross_attn_fwd")
+
+
+def agg_cache_bytes(cache: agg_cache) -> int:
+    nbytes = ctypes.c_size_t(0)
+    _check(lib().agg_cache_bytes(ctypes.byref(cache), ctypes.byref(nbytes)), "agg_cache_bytes")
+    return nbytes.value
+
+
+def agg_cache_append(cache, shape, rope, q_norm, k_norm, pos, Q, q_stride, K, k_stride, V, v_stride, start=None,
+                     counts=None, lens=None, Qr=None, stream=None):
+    _check(lib().agg_cache_append(ctypes.byref(cache), ctypes.byref(shape), _ref(rope), _ref(q_norm), _ref(k_norm),
+                                  _ptr(pos), _ptr(Q), int(q_stride), _ptr(K), int(k_stride), _ptr(V), int(v_stride),
+                                  _ptr(start), _ptr(counts), _ptr(lens), _ptr(Qr), _stream(stream)),
+           "agg_cache_append")
+
+
+def agg_cache_attn_fwd(cache, cross, Q, q_stride, O, lse=None, workspace=None, workspace_bytes=0, stream=None):
+    _check(lib().agg_cache_attn_fwd(ctypes.byref(cache), ctypes.byref(cross), _ptr(Q), int(q_stride), _ptr(O),
+                                    _ptr(lse), _ptr(workspace), int(workspace_bytes), _stream(stream)),
+           "agg_cache_attn_fwd")

@@ -573,6 +573,191 @@ int make_mx4_args(int64_t rows, int32_t N, int32_t K, const agg_mx4_linear* l, c
   return AGG_OK;
 }
 
+// ---- attention to keys of another length, the paged cache ----
+bool misaligned4(const void* p) { return ((uintptr_t)p & 3u) != 0; }
+
+// the sizes of a call, without its pointers
+int check_cross(const agg_cross* c) {
+  if (!c) return AGG_ERR_NULL;
+  if (c->B < 1 || c->NQ < 0 || c->NK < 0 || c->H < 1 || c->H_kv < 1 || c->D < 1 || c->H % c->H_kv != 0) return AGG_ERR_SHAPE;
+  if (!(c->scale > 0.0f) || !(c->scale < 1e30f)) return AGG_ERR_SHAPE;
+  if (c->D != kHeadDim) return AGG_ERR_UNSUPPORTED;
+  // rows of a key head and key numbers are counted with 31 bits, a tensor stays under 2^60 bytes
+  constexpr int64_t kMost = INT32_MAX - 512;
+  if (c->NK > kMost || (int64_t)c->NQ * (c->H / c->H_kv) > kMost || (int64_t)c->B * c->H > INT32_MAX) return AGG_ERR_OVERFLOW;
+  const int64_t longest = c->NQ > c->NK ? c->NQ : c->NK;
+  if (longest > 0 && (int64_t)c->B * c->H > ((int64_t)1 << 40) / longest) return AGG_ERR_OVERFLOW;
+  return AGG_OK;
+}
+
+int check_cache(const agg_cache* c) {
+  if (!c) return AGG_ERR_NULL;
+  if (c->n_pages < 1 || c->H < 1 || c->D < 1 || c->B < 1 || c->max_pages < 1) return AGG_ERR_SHAPE;
+  if (c->D != kHeadDim) return AGG_ERR_UNSUPPORTED;
+  // rows of a sequence are counted with 31 bits, a pool stays under 2^60 bytes
+  if (c->max_pages > (INT32_MAX - 512) / kTileRows || (int64_t)c->n_pages * c->H > ((int64_t)1 << 46)) return AGG_ERR_OVERFLOW;
+  return AGG_OK;
+}
+uint64_t pool_bytes(const agg_cache* c) { return (uint64_t)c->n_pages * c->H * kTileElems * 2; }
+uint64_t table_bytes(const agg_cache* c) { return (uint64_t)c->B * c->max_pages * 4; }
+int check_cache_pointers(const agg_cache* c) {
+  if (!c->Kc || !c->Vc || !c->pages) return AGG_ERR_NULL;
+  if (misaligned(c->Kc) || misaligned(c->Vc) || misaligned4(c->pages)) return AGG_ERR_ALIGN;
+  return AGG_OK;
+}
+
+// a token's distance from the next, 0 meaning contiguous; bytes of the tensor from its first element to its last
+int token_stride(int64_t given, int64_t tokens, int64_t heads, int64_t* stride, uint64_t* bytes) {
+  const int64_t C = heads * kHeadDim;
+  *stride = given ? given : C;
+  *bytes = 0;
+  if (*stride < C || *stride % 8 != 0) return AGG_ERR_SHAPE;
+  if (tokens < 1) return AGG_OK;
+  if (*stride > ((int64_t)1 << 59) / tokens) return AGG_ERR_OVERFLOW;
+  *bytes = ((uint64_t)(tokens - 1) * *stride + C) * 2;
+  return AGG_OK;
+}
+
+struct Bytes {
+  const void* p;
+  uint64_t n;
+};
+
+// Everything the two attention calls check; AGG_OK with *a filled in.  cache: keys and values lie there, K and V are not given.
+int make_cross_args(const agg_cross* c, const agg_cache* cache, const void* Q, int64_t q_stride, const void* K,
+                    int64_t k_stride, const void* V, int64_t v_stride, void* O, float* lse, void* workspace,
+                    size_t workspace_bytes, CrossArgs* a) {
+  int rc = check_cross(c);
+  if (rc != AGG_OK) return rc;
+  memset(a, 0, sizeof *a);
+  if (cache) {
+    if ((rc = check_cache(cache)) != AGG_OK) return rc;
+    if (c->B != cache->B || c->H_kv != cache->H || c->NK > (int64_t)cache->max_pages * kTileRows) return AGG_ERR_SHAPE;
+  }
+  const int64_t queries = (int64_t)c->B * c->NQ, keys = (int64_t)c->B * c->NK;
+  uint64_t q_bytes, k_bytes = 0, v_bytes = 0;
+  if ((rc = token_stride(q_stride, queries, c->H, &a->q_stride, &q_bytes)) != AGG_OK) return rc;
+  if (!cache) {
+    if ((rc = token_stride(k_stride, keys, c->H_kv, &a->k_stride, &k_bytes)) != AGG_OK) return rc;
+    if ((rc = token_stride(v_stride, keys, c->H_kv, &a->v_stride, &v_bytes)) != AGG_OK) return rc;
+  }
+  if (queries > 0 && (!Q || !O)) return AGG_ERR_NULL;
+  if (cache) {
+    if ((rc = check_cache_pointers(cache)) != AGG_OK) return rc;
+  } else if (keys > 0 && (!K || !V)) {
+    return AGG_ERR_NULL;
+  }
+  if (misaligned(Q) || misaligned(K) || misaligned(V) || misaligned(O) || misaligned(workspace) || misaligned4(lse) ||
+      misaligned4(c->q_lens) || misaligned4(c->k_lens))
+    return AGG_ERR_ALIGN;
+  const size_t need = cross_partial_floats(c->B, c->NQ, c->NK, c->H, c->H_kv) * sizeof(float);
+  if (need > 0 && !workspace) return AGG_ERR_NULL;
+  if (workspace_bytes < need) return AGG_ERR_WORKSPACE;
+  // what the call writes may overlap nothing else of it
+  const Bytes out[] = {{O, (uint64_t)queries * c->H * kHeadDim * 2}, {lse, (uint64_t)queries * c->H * 4}, {workspace, need}};
+  const Bytes in[] = {{Q, q_bytes}, {K, k_bytes}, {V, v_bytes}, {c->q_lens, (uint64_t)c->B * 4}, {c->k_lens, (uint64_t)c->B * 4},
+                      {cache ? cache->Kc : nullptr, cache ? pool_bytes(cache) : 0},
+                      {cache ? cache->Vc : nullptr, cache ? pool_bytes(cache) : 0},
+                      {cache ? cache->pages : nullptr, cache ? table_bytes(cache) : 0}};
+  for (const Bytes& o : out) {
+    for (const Bytes& i : in)
+      if (overlap(o.p, o.n, i.p, i.n)) return AGG_ERR_SHAPE;
+    for (const Bytes& other : out)
+      if (&other != &o && overlap(o.p, o.n, other.p, other.n)) return AGG_ERR_SHAPE;
+  }
+  a->B = c->B;
+  a->NQ = c->NQ;
+  a->NK = c->NK;
+  a->H = c->H;
+  a->H_kv = c->H_kv;
+  a->group = c->H / c->H_kv;
+  a->scale2 = c->scale * 1.4426950408889634f;
+  a->Q = (const uint16_t*)Q;
+  a->K = (const uint16_t*)K;
+  a->V = (const uint16_t*)V;
+  if (cache) {
+    a->Kc = (const uint16_t*)cache->Kc;
+    a->Vc = (const uint16_t*)cache->Vc;
+    a->pages = cache->pages;
+    a->max_pages = cache->max_pages;
+    a->n_pages = cache->n_pages;
+  }
+  a->q_lens = c->q_lens;
+  a->k_lens = c->k_lens;
+  a->O = (uint16_t*)O;
+  a->lse = lse;
+  a->partial = (float*)workspace;
+  return AGG_OK;
+}
+
+// Everything agg_cache_append checks.  The shape's heads count for the queries alone: without them the cache's stand in.
+int make_append_args(const agg_cache* c, const agg_shape* shape, const agg_rope* rope, const agg_norm* q_norm,
+                     const agg_norm* k_norm, const int32_t* pos, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
+                     const void* V, int64_t v_stride, const int32_t* start, const int32_t* counts, int32_t* lens, void* Qr,
+                     AppendArgs* a) {
+  int rc = check_cache(c);
+  if (rc != AGG_OK) return rc;
+  if (!shape) return AGG_ERR_NULL;
+  agg_shape s = *shape;
+  if (!Q) s.H = c->H;
+  Geom g;
+  if ((rc = make_geom(&s, &g, true)) != AGG_OK) return rc;
+  if (s.B != c->B || s.H % c->H != 0) return AGG_ERR_SHAPE;
+  memset(a, 0, sizeof *a);
+  RopeArgs* r = &a->r;
+  if ((rc = make_rope(rope, r)) != AGG_OK) return rc;
+  if ((rc = make_norm(q_norm, &r->norm[0])) != AGG_OK) return rc;
+  if ((rc = make_norm(k_norm, &r->norm[1])) != AGG_OK) return rc;
+  if ((Q == nullptr) != (Qr == nullptr) || !K || !V) return AGG_ERR_NULL;
+  if ((rc = check_cache_pointers(c)) != AGG_OK) return rc;
+  if (misaligned(Q) || misaligned(Qr) || misaligned(K) || misaligned(V) || misaligned4(pos) || misaligned4(start) ||
+      misaligned4(counts) || misaligned4(lens))
+    return AGG_ERR_ALIGN;
+  if (!pos && rope) {
+    const int64_t side = g.n_h > g.n_w ? g.n_h : g.n_w;
+    if ((int64_t)rope->t0 + g.N > INT32_MAX || (int64_t)rope->patch0 + side > INT32_MAX) return AGG_ERR_OVERFLOW;
+  }
+  r->total = (int64_t)g.B * g.NQ;
+  uint64_t q_bytes, k_bytes, v_bytes;
+  if ((rc = token_stride(q_stride, r->total, g.H, &r->stride[0], &q_bytes)) != AGG_OK) return rc;
+  if ((rc = token_stride(k_stride, r->total, c->H, &r->stride[1], &k_bytes)) != AGG_OK) return rc;
+  if ((rc = token_stride(v_stride, r->total, c->H, &a->v_stride, &v_bytes)) != AGG_OK) return rc;
+  const uint64_t qr_bytes = (uint64_t)r->total * g.H * kHeadDim * 2;
+  const bool in_place = Q == Qr && r->stride[0] == (int64_t)g.H * kHeadDim;
+  const Bytes out[] = {{c->Kc, pool_bytes(c)}, {c->Vc, pool_bytes(c)}, {lens, (uint64_t)c->B * 4}, {Qr, Qr ? qr_bytes : 0}};
+  const Bytes in[] = {{Q, Q ? q_bytes : 0}, {K, k_bytes}, {V, v_bytes}, {pos, (uint64_t)r->total * 12}, {start, (uint64_t)c->B * 4},
+                      {counts, (uint64_t)c->B * 4}, {c->pages, table_bytes(c)}};
+  for (const Bytes& o : out) {
+    for (const Bytes& i : in)
+      if (!(in_place && o.p == Qr && i.p == Q) && overlap(o.p, o.n, i.p, i.n)) return AGG_ERR_SHAPE;
+    for (const SeamNorm& n : r->norm)
+      if (overlap_norm(o.p, o.n, n, kHeadDim)) return AGG_ERR_SHAPE;
+    for (const Bytes& other : out)
+      if (&other != &o && overlap(o.p, o.n, other.p, other.n)) return AGG_ERR_SHAPE;
+  }
+  r->in[0] = (const uint16_t*)Q;
+  r->in[1] = (const uint16_t*)K;
+  r->out[0] = (uint16_t*)Qr;
+  r->pos = pos;
+  r->NQ = g.NQ;
+  r->H = g.H;
+  r->L = g.L;
+  r->P = g.P;
+  r->n_w = g.n_w;
+  a->V = (const uint16_t*)V;
+  a->Kc = (uint16_t*)c->Kc;
+  a->Vc = (uint16_t*)c->Vc;
+  a->pages = c->pages;
+  a->start = start;
+  a->counts = counts;
+  a->lens = lens;
+  a->B = c->B;
+  a->H_kv = c->H;
+  a->max_pages = c->max_pages;
+  a->n_pages = c->n_pages;
+  return AGG_OK;
+}
+
 }  // namespace
 
 int agg_rope_fwd(const agg_shape* shape, const agg_rope* rope, const agg_norm* q_norm,
@@ -635,6 +820,48 @@ int agg_mx4_linear_fwd(int64_t rows, int32_t N, int32_t K, const agg_mx4_linear*
   const int rc = make_mx4_args(rows, N, K, linear, codes, scales, &a);
   if (rc != AGG_OK || rows == 0) return rc;
   return launch_mx4_linear(a, (hipStream_t)hip_stream) == hipSuccess ? AGG_OK : AGG_ERR_LAUNCH;
+}
+
+size_t agg_cross_workspace_bytes(const agg_cross* cross) {
+  if (check_cross(cross) != AGG_OK) return 0;
+  return cross_partial_floats(cross->B, cross->NQ, cross->NK, cross->H, cross->H_kv) * sizeof(float);
+}
+
+int agg_cross_attn_fwd(const agg_cross* cross, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
+                       const void* V, int64_t v_stride, void* O, float* lse, void* workspace,
+                       size_t workspace_bytes, void* hip_stream) {
+  CrossArgs a;
+  const int rc = make_cross_args(cross, nullptr, Q, q_stride, K, k_stride, V, v_stride, O, lse, workspace, workspace_bytes, &a);
+  if (rc != AGG_OK || a.NQ == 0) return rc;
+  return launch_cross(a, (hipStream_t)hip_stream) == hipSuccess ? AGG_OK : AGG_ERR_LAUNCH;
+}
+
+int agg_cache_bytes(const agg_cache* cache, size_t* bytes) {
+  const int rc = check_cache(cache);
+  if (rc != AGG_OK) return rc;
+  if (!bytes) return AGG_ERR_NULL;
+  *bytes = (size_t)pool_bytes(cache);
+  return AGG_OK;
+}
+
+int agg_cache_append(const agg_cache* cache, const agg_shape* shape, const agg_rope* rope, const agg_norm* q_norm,
+                     const agg_norm* k_norm, const int32_t* pos, const void* Q, int64_t q_stride, const void* K,
+                     int64_t k_stride, const void* V, int64_t v_stride, const int32_t* start, const int32_t* counts,
+                     int32_t* lens, void* Qr, void* hip_stream) {
+  AppendArgs a;
+  const int rc = make_append_args(cache, shape, rope, q_norm, k_norm, pos, Q, q_stride, K, k_stride, V, v_stride, start, counts,
+                                  lens, Qr, &a);
+  if (rc != AGG_OK) return rc;
+  return launch_append(a, (hipStream_t)hip_stream) == hipSuccess ? AGG_OK : AGG_ERR_LAUNCH;
+}
+
+int agg_cache_attn_fwd(const agg_cache* cache, const agg_cross* cross, const void* Q, int64_t q_stride, void* O,
+                       float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (!cache) return AGG_ERR_NULL;
+  CrossArgs a;
+  const int rc = make_cross_args(cross, cache, Q, q_stride, nullptr, 0, nullptr, 0, O, lse, workspace, workspace_bytes, &a);
+  if (rc != AGG_OK || a.NQ == 0) return rc;
+  return launch_cross(a, (hipStream_t)hip_stream) == hipSuccess ? AGG_OK : AGG_ERR_LAUNCH;
 }
 
 // ---- one global-attention block --------------------------------------------------------

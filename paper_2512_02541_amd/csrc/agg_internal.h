@@ -224,6 +224,42 @@ struct Mx4LinearArgs {
 };
 hipError_t launch_mx4_linear(const Mx4LinearArgs& args, hipStream_t st);
 
+// Attention to keys of another length (agg_cross_attn_fwd, agg_cache_attn_fwd).  Rows of a (batch element, key head) pair: its
+// queries by the heads that share the key head, row = query * group + head in the group.
+struct CrossArgs {
+  int32_t B, NQ, NK, H, H_kv, group;
+  float scale2;  // scale * log2(e)
+  const uint16_t *Q, *K, *V;
+  int64_t q_stride, k_stride, v_stride;
+  // cache: the pools and the page table (null: K and V where they are)
+  const uint16_t *Kc, *Vc;
+  const int32_t* pages;
+  int32_t max_pages, n_pages;
+  const int32_t *q_lens, *k_lens;
+  uint16_t* O;
+  float* lse;
+  float* partial;  // workspace
+};
+// floats of workspace
+size_t cross_partial_floats(int64_t B, int64_t NQ, int64_t NK, int64_t H, int64_t H_kv);
+hipError_t launch_cross(const CrossArgs& args, hipStream_t st);
+
+// New tokens of a cache (agg_cache_append).
+struct AppendArgs {
+  RopeArgs r;      // [0]: queries to row-major Qr; [1]: keys, whose `out` is not used
+  const uint16_t* V;
+  int64_t v_stride;
+  uint16_t *Kc, *Vc;
+  const int32_t* pages;
+  const int32_t *start, *counts;
+  int32_t* lens;
+  int32_t B, H_kv, max_pages, n_pages;
+  // set by launch_append: pieces of 32 rows of a sequence and workgroups that share the heads of one, for keys and for queries
+  int64_t k_items, q_items;
+  int32_t k_units, q_units, k_parts, q_parts;
+};
+hipError_t launch_append(const AppendArgs& args, hipStream_t st);
+
 int mean_chunks(const Geom& g);  // number of partial-sum blocks the mean kernel uses
 
 // Device array inside the library that stands in for the caller's workspace in

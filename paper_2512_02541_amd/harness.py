@@ -286,3 +286,38 @@ def block_ex_forward(shape, mode, wts, options, x):
     n = _buf(tuple(x.shape), x.dtype, x.device, "block n") if options.residual.pre.kind else None
     agg.agg_global_block_ex_fwd(shape, mode, cw, options, x, y, n, ws, nws)
     return y, n
+
+
+# ---- keys of another length, the paged cache -------------------------------------------------
+def _cross_out(cross, device):
+    o = _buf((cross.B, cross.NQ, cross.H, 64), torch.bfloat16, device, "cross O")
+    lse = _buf((cross.B, cross.H, cross.NQ), torch.float32, device, "cross lse")
+    o.view(torch.int16).fill_(0x7FC1)   # NaN: rows that a call leaves alone keep it
+    lse.fill_(float("nan"))
+    n = agg.agg_cross_workspace_bytes(cross)
+    ws = _buf(n, torch.uint8, device, "cross workspace") if n else None
+    if n:
+        ws.fill_(0xFF)
+    return o, lse, ws, n
+
+
+def cross_forward(cross, Q, K, V, q_stride=0, k_stride=0, v_stride=0):
+    """O and lse of attention to K and V where they are; rows that do not exist hold NaN."""
+    o, lse, ws, n = _cross_out(cross, Q.device)
+    agg.agg_cross_attn_fwd(cross, Q, q_stride, K, k_stride, V, v_stride, o, lse, ws, n)
+    return o, lse
+
+
+def cache_forward(cache, cross, Q, q_stride=0):
+    """O and lse of attention over a cache."""
+    o, lse, ws, n = _cross_out(cross, Q.device)
+    agg.agg_cache_attn_fwd(cache, cross, Q, q_stride, o, lse, ws, n)
+    return o, lse
+
+
+def make_pools(n_pages, H, device, fill=0x7FC1):
+    """Two pools of a cache, filled with a bit pattern (NaN)."""
+    pools = [_buf((n_pages, H, 4096), torch.bfloat16, device, "pool " + name) for name in ("K", "V")]
+    for p in pools:
+        p.view(torch.int16).fill_(fill)
+    return pools
