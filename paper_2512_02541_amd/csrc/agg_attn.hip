@@ -426,40 +426,6 @@ __device__ __forceinline__ bool attend(const AttnArgs& p, uint16_t* tiles, uint3
   return true;
 }
 
-// position in a launch list of n tiles per pair -> (pair, tile of the pair).  Consecutive ids go
-// to consecutive XCDs.  Whole pairs are dealt out one per XCD, so that an XCD streams one
-// key/value set at a time through its own L2; the npairs % 8 pairs that are left share the XCDs
-// between them, each XCD taking an equal, contiguous run of their tiles.  (Dealing those out whole
-// as well left XCDs idle: ordinary attention over 24 frames of 28x37 patches with 12 heads took
-// 2.12 ms, with the shared run 1.52.)
-struct TileList {
-  int n;         // tiles per pair
-  int whole;     // tiles of an XCD's whole pairs
-  int rest;      // tiles of an XCD's run over the remaining pairs
-  int groups;    // workgroups of the list
-};
-__host__ __device__ inline TileList tile_list(int npairs, int n) {
-  TileList l;
-  l.n = n;
-  l.whole = npairs / kXcds * n;
-  l.rest = (npairs % kXcds * n + kXcds - 1) / kXcds;
-  l.groups = kXcds * (l.whole + l.rest);
-  return l;
-}
-__device__ __forceinline__ bool list_tile(const TileList& l, int npairs, int bid, int& pair, int& i) {
-  const int xcd = bid % kXcds;
-  const int seq = bid / kXcds;
-  if (seq < l.whole) {
-    pair = (seq / l.n) * kXcds + xcd;
-    i = seq % l.n;
-  } else {
-    const int u = seq - l.whole + xcd * l.rest;
-    if (u >= npairs % kXcds * l.n) return false;  // uniform for the whole workgroup
-    pair = npairs / kXcds * kXcds + u / l.n;
-    i = u % l.n;
-  }
-  return true;
-}
 __host__ __device__ inline TileList first_list(const TilePlan& t, int npairs) {
   return tile_list(npairs, t.n_full + (t.tails_last ? 0 : t.n_tail));
 }

@@ -174,7 +174,13 @@ __device__ __forceinline__ void exp_unit_sum(const f32x4 (&S)[2 * kJ], Frag (&P)
 // keys of one channel per lane) come from the transposing read ds_read_b64_tr_b16, which hands
 // lane i of a 16-lane group the i-th 16-bit column of the four 8-byte rows the group's lanes
 // 4j .. 4j+3 point at.
-enum { kSrcCompact = 0, kSrcRows = 1, kSrcIndexed = 2 };
+//   kSrcStrided: consecutive rows of K and V, each with a distance of its own, whose number is a device's value (attention
+//                to keys of another length).
+//   kSrcPaged:   fragment-order tiles again, each found through a page table.
+// The last two may end anywhere in memory that holds something else: their values are masked behind the last key, since 0
+// times what lies there may be no number.
+enum { kSrcCompact = 0, kSrcRows = 1, kSrcIndexed = 2, kSrcStrided = 3, kSrcPaged = 4 };
+constexpr bool fragment_order(int src) { return src == kSrcCompact || src == kSrcPaged; }
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
@@ -224,7 +230,7 @@ __device__ __forceinline__ FragAddr frag_addr(int lane) {
 template <int kSrc>
 __device__ __forceinline__ void load_k_frags(const u32x4* __restrict__ lds, int buf, int kb,
                                              const FragAddr& f, Frag (&a)[4]) {
-  if (kSrc == kSrcCompact) {
+  if (fragment_order(kSrc)) {
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -240,7 +246,7 @@ __device__ __forceinline__ void load_k_frags(const u32x4* __restrict__ lds, int 
 template <int kSrc>
 __device__ __forceinline__ void load_v_frags(const u32x4* __restrict__ lds, int buf, int kb,
                                              const FragAddr& f, Frag (&v)[4]) {
-  if (kSrc == kSrcCompact) {
+  if (fragment_order(kSrc)) {
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt)
       v[dt].u = lds[(kLdsTiles + buf) * kChunks + kb * 256 + dt * 16 + f.vc];
@@ -261,6 +267,18 @@ __device__ __forceinline__ void load_v_frags(const u32x4* __restrict__ lds, int 
   }
 }
 
+// Values of keys behind the last one, of 32 whose first `left` exist, become zero.
+__device__ __forceinline__ void mask_values(Frag (&v)[4], int left, int G) {
+  const int k0 = 16 * (G >> 1) + 4 * (G & 1);  // a lane's eight keys: k0 .. + 3, k0 + 8 .. + 11
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int key = k0 + (i >> 1) * 8 + (i & 1) * 2;
+    const uint32_t mask = (key < left ? 0xFFFFu : 0u) | (key + 1 < left ? 0xFFFF0000u : 0u);
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt) v[dt].u[i] &= mask;
+  }
+}
+
 // What a workgroup needs to know about its key/value source.
 struct KvSource {
   const uint16_t *k, *v;   // compact: tile 0 of this (batch, head); rows: token 0's row of this head
@@ -268,6 +286,10 @@ struct KvSource {
   int64_t rows;            // number of keys (M, or the sequence length)
   uint32_t row_bytes;      // rows: distance between consecutive tokens' rows (H * 128)
   uint32_t max_token;      // indexed: largest valid token id (N*L - 1)
+  uint32_t v_row_bytes;    // strided: row_bytes of V
+  ScalarInts pages;        // paged: the page numbers of this workgroup's tiles; k, v: head 0's tile of page 0
+  int32_t tiles, last_page;  // paged: how many, the largest page number
+  int64_t page_elems, head_elems;  // paged: from a page to the next, from head 0 to this one
 };
 
 // Issues the asynchronous copy of tile t into LDS buffer `buf`.  Every wavefront lands 64
@@ -293,6 +315,7 @@ struct TileCopier {
   uint32_t list_at;        // byte offset of this lane's id for the tile after the next
   uint32_t id;             // its id for the tile after the next to be copied
   uint32_t from[2];        // next tile to be copied: byte offset of the rows this lane fetches
+  int32_t page;            // paged: page of the next tile to be copied
 
   __device__ __forceinline__ void init(const KvSource& s, const u32x4* lds, int tid, int wave) {
     src = s;
@@ -306,7 +329,7 @@ struct TileCopier {
     const uint32_t c = slot & 7;
     const uint32_t ck = (c ^ k_swizzle(row)) * 16u;
     const uint32_t cv = (c ^ (4u * ((row >> 1) & 1))) * 16u;
-    if (kSrc == kSrcCompact) {
+    if (fragment_order(kSrc)) {
       // K: the LDS slot of a key has bits 3 and 4 of the key number exchanged (frag_addr)
       const uint32_t key = slot & 31u;
       const uint32_t swapped = (key & 7u) | ((key & 8u) << 1) | ((key & 16u) >> 1);
@@ -315,6 +338,9 @@ struct TileCopier {
     } else if (kSrc == kSrcRows) {
       vk = row * s.row_bytes + ck;
       vv = row * s.row_bytes + cv;
+    } else if (kSrc == kSrcStrided) {
+      vk = row * s.row_bytes + ck;
+      vv = row * s.v_row_bytes + cv;
     } else {
       vk = ck;
       vv = cv;
@@ -327,6 +353,7 @@ struct TileCopier {
       spread_ids();
       fetch_ids();
     }
+    if (kSrc == kSrcPaged) page = s.pages[0];
   }
   __device__ __forceinline__ void fetch_ids() {  // rows past the end repeat the last one; masked later
     const uint32_t at = min(list_at, ((uint32_t)src.rows - 1u) * 4u);
@@ -374,6 +401,35 @@ struct TileCopier {
       }
       knext += 2 * half;
       vnext += 2 * half;
+    } else if (kSrc == kSrcStrided) {
+      const size_t k_half = (size_t)(kTileRows / 2) * (src.row_bytes / 2), v_half = (size_t)(kTileRows / 2) * (src.v_row_bytes / 2);
+      if ((tnext + 1) * kTileRows <= src.rows) {
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+          dma16(knext + hh * k_half, vk, mk + hh * kAttnThreads * 16);
+          dma16(vnext + hh * v_half, vv, mv + hh * kAttnThreads * 16);
+        }
+      } else {  // last, partial tile: rows past the end repeat the last one; masked later
+        const uint32_t last = (uint32_t)(src.rows - 1 - tnext * kTileRows);
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+          const uint32_t r = row + hh * (kTileRows / 2);
+          const uint32_t beyond = min(r, last) - row;  // (wraps where the row is before this lane's)
+          dma16(knext, vk + beyond * src.row_bytes, mk + hh * kAttnThreads * 16);
+          dma16(vnext, vv + beyond * src.v_row_bytes, mv + hh * kAttnThreads * 16);
+        }
+      }
+      knext += 2 * k_half;
+      vnext += 2 * v_half;
+    } else if (kSrc == kSrcPaged) {
+      // the page's number came a tile ahead; one outside the pool is read as the first or the last page
+      const int64_t at = min(max(page, 0), src.last_page) * src.page_elems + src.head_elems;
+#pragma unroll
+      for (int hh = 0; hh < 2; ++hh) {
+        dma16(src.k + at + hh * (kTileElems / 2), vk, mk + hh * kAttnThreads * 16);
+        dma16(src.v + at + hh * (kTileElems / 2), vv, mv + hh * kAttnThreads * 16);
+      }
+      page = src.pages[min((int32_t)tnext + 1, src.tiles - 1)];
     } else {
 #pragma unroll
       for (int hh = 0; hh < 2; ++hh) {
@@ -486,7 +542,10 @@ __device__ __forceinline__ void tile_steps(Wave<kQB, kJ>& w, const u32x4* __rest
 
     // ---- matrix core, part 2: P V of unit sg - 1 ----
     pv_unit<kGen, kQB, kJ>(w, pq);
-    if (qb == 0) load_v_frags<kSrc>(lds, cur, kb, fa, w.v);  // the previous block is done with them
+    if (qb == 0) {  // the previous block is done with them
+      load_v_frags<kSrc>(lds, cur, kb, fa, w.v);
+      if (kSrc >= kSrcStrided && kLast && valid < kTileRows) mask_values(w.v, valid - 32 * kb, G);
+    }
 #pragma unroll
     for (int j = 0; j < kJ; ++j) w.P[j] = Pn[j];
     // Issue order inside the step: MFMAs and exponentials alternate one by one, a conversion
@@ -614,6 +673,41 @@ __device__ __forceinline__ bool key_loop(Wave<kQB, kJ>& w, u32x4* __restrict__ l
   // last tile (runtime buffer number), then the P V of its last unit
   tile_steps<kSrc, true, kGen, kQB, kJ>(w, lds, cur, 0, last_valid, fa, G);
   pv_unit<kGen, kQB, kJ>(w, kQB - 1);
+  return true;
+}
+
+// position in a launch list of n tiles per pair -> (pair, tile of the pair).  Consecutive ids go
+// to consecutive XCDs.  Whole pairs are dealt out one per XCD, so that an XCD streams one
+// key/value set at a time through its own L2; the npairs % 8 pairs that are left share the XCDs
+// between them, each XCD taking an equal, contiguous run of their tiles.  (Dealing those out whole
+// as well left XCDs idle: ordinary attention over 24 frames of 28x37 patches with 12 heads took
+// 2.12 ms, with the shared run 1.52.)
+struct TileList {
+  int n;         // tiles per pair
+  int whole;     // tiles of an XCD's whole pairs
+  int rest;      // tiles of an XCD's run over the remaining pairs
+  int groups;    // workgroups of the list
+};
+__host__ __device__ inline TileList tile_list(int npairs, int n) {
+  TileList l;
+  l.n = n;
+  l.whole = npairs / kXcds * n;
+  l.rest = (npairs % kXcds * n + kXcds - 1) / kXcds;
+  l.groups = kXcds * (l.whole + l.rest);
+  return l;
+}
+__device__ __forceinline__ bool list_tile(const TileList& l, int npairs, int bid, int& pair, int& i) {
+  const int xcd = bid % kXcds;
+  const int seq = bid / kXcds;
+  if (seq < l.whole) {
+    pair = (seq / l.n) * kXcds + xcd;
+    i = seq % l.n;
+  } else {
+    const int u = seq - l.whole + xcd * l.rest;
+    if (u >= npairs % kXcds * l.n) return false;  // uniform for the whole workgroup
+    pair = npairs / kXcds * kXcds + u / l.n;
+    i = u % l.n;
+  }
   return true;
 }
 

@@ -6,8 +6,6 @@ namespace agg {
 
 namespace {
 
-typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
-
 // keys and queries of batch element b, whatever the caller's lengths hold
 __device__ __forceinline__ int cross_keys(const CrossArgs& a, int b) {
   return a.k_lens ? min(max(((ScalarInts)a.k_lens)[b], 0), a.NK) : a.NK;
@@ -31,6 +29,10 @@ __device__ __forceinline__ int64_t partial_row(const CrossArgs& a, int64_t pairs
   return ((int64_t)split * pairs + pair) * ((int64_t)a.NQ * a.group) + row;
 }
 
+__device__ __forceinline__ float* partial_sums(const CrossArgs& a, int64_t pairs, int splits) {
+  return a.partial + (int64_t)splits * pairs * a.NQ * a.group * kHeadDim;
+}
+
 __device__ __forceinline__ u32x2 pack4(f32x4 v) { return u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}; }
 
 // A finished row: four channels a thread.  m: the reference in base 2, l: the sum, o: sum of exp2(logit - m) v.
@@ -51,13 +53,13 @@ __device__ __forceinline__ void store_row(const CrossArgs& a, int b, int hk, uin
 // values through LDS), with the running maximum and sum of an online softmax; the wavefronts of a workgroup, and the
 // workgroups that share a pair's keys, are joined at the end by their references.
 // ---------------------------------------------------------------------------
-constexpr int few_threads(int tiles) { return 64 * (tiles == 4 ? 4 : kFewWaves); }
+constexpr int kFewThreads = 64 * kFewWaves;
 constexpr int kRowFloats = kHeadDim + 4;  // of a row in LDS, padded
 
 template <bool kPaged, int kJ>
-__global__ __launch_bounds__(few_threads(kJ), kJ == 1 ? 4 : 2) void cross_few_kernel(CrossArgs a, CrossPlan plan, int64_t pairs,
+__global__ __launch_bounds__(kFewThreads, kJ == 1 ? 4 : 2) void cross_few_kernel(CrossArgs a, CrossPlan plan, int64_t pairs,
                                                                                     int64_t first) {
-  constexpr int kW = few_threads(kJ) / 64;
+  constexpr int kW = kFewWaves;
   __shared__ __align__(16) float lds[kW * 16 * kJ * (kRowFloats + 2)];
   static_assert(sizeof(lds) >= kW * 4096, "a block of values for each wavefront");
   const int lane = threadIdx.x & 63, c = lane & 15, G = lane >> 4;
@@ -134,16 +136,7 @@ __global__ __launch_bounds__(few_threads(kJ), kJ == 1 ? 4 : 2) void cross_few_ke
     if constexpr (kPaged) {
 #pragma unroll
       for (int dt = 0; dt < 4; ++dt) V[dt].u = x.v[dt];
-      if (left < kKeyBlock) {  // what lies behind the last key may be anything: 0 times it may be no number
-        const int k0 = 16 * (G >> 1) + 4 * (G & 1);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int key = k0 + (i >> 1) * 8 + (i & 1) * 2;
-          const uint32_t mask = (key < left ? 0xFFFFu : 0u) | (key + 1 < left ? 0xFFFF0000u : 0u);
-#pragma unroll
-          for (int dt = 0; dt < 4; ++dt) V[dt].u[i] &= mask;
-        }
-      }
+      if (left < kKeyBlock) mask_values(V, left, G);
     } else {
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
       __builtin_amdgcn_wave_barrier();
@@ -251,45 +244,337 @@ __global__ __launch_bounds__(few_threads(kJ), kJ == 1 ? 4 : 2) void cross_few_ke
     } else {
       const int64_t at = partial_row(a, pairs, split, pair, r0 + row);
       *reinterpret_cast<f32x4*>(a.partial + at * kHeadDim + 4 * quad) = o;
-      if (quad == 0) {
-        float* const s = a.partial + (int64_t)plan.splits * pairs * a.NQ * a.group * kHeadDim + at * 2;
-        *reinterpret_cast<f32x2*>(s) = f32x2{hi > lo ? ref : -INFINITY, total};
-      }
+      if (quad == 0)
+        *reinterpret_cast<f32x2*>(partial_sums(a, pairs, plan.splits) + at * 2) = f32x2{hi > lo ? ref : -INFINITY, total};
     }
   }
 }
 
-// Joins the splits' results: sixteen threads a row.
+// ---------------------------------------------------------------------------
+// Many rows a pair: the pipeline of agg_attn.hip over keys that end where the sequence's do, bound like it by the matrix core
+// and the vector ALU together.  256 rows a workgroup, 128 or 192 in a pair's last one; few pairs are shared out along the
+// keys too, each workgroup leaving its sums without (fast path) or with (general path) a reference in the workspace.  A workgroup whose
+// sums leave the fast path's range redoes its rows in place, 128 at a time.
+// ---------------------------------------------------------------------------
+namespace {
+
+// One workgroup's rows row_begin .. row_end - 1 of pair (b, hk) over its split's keys, by one of the two paths.  Returns false, without
+// storing anything, when the fast path met a row it cannot handle.
+template <int kSrc, bool kGen, int kQB, int kJ>
+__device__ __forceinline__ bool attend_cross(const CrossArgs& p, const CrossPlan& plan, int64_t pairs, uint16_t* tiles, uint32_t* votes,
+                                             int64_t pair, int split, uint32_t row_begin, uint32_t row_end) {
+  constexpr int kWaveQ = wave_queries(kQB, kJ);
+  // (opaque on the general path, so that it holds nothing of the fast path's: agg_attn.hip)
+  int tid = threadIdx.x;
+  if (kGen) asm volatile("" : "+v"(tid));
+  u32x4* lds = reinterpret_cast<u32x4*>(tiles);
+  const int lane = tid & 63, wave = tid >> 6, c = lane & 15, G = lane >> 4;
+  const FragAddr fa = frag_addr(lane);
+  const int b = (int)(pair / p.H_kv), hk = (int)(pair % p.H_kv);
+
+  // this workgroup's key tiles
+  const int n = cross_keys(p, b);
+  const int64_t all = ((int64_t)n + kTileRows - 1) / kTileRows;
+  const int skip = (int)(all * split / plan.splits);
+  const int ntiles = (int)(all * (split + 1) / plan.splits) - skip;
+  const int rows_here = min(n - skip * kTileRows, ntiles * kTileRows);
+  const int last_valid = rows_here - (ntiles - 1) * kTileRows;  // 1..64
+  KvSource src;
+  src.rows = rows_here;
+  if (kSrc == kSrcPaged) {
+    src.k = p.Kc;
+    src.v = p.Vc;
+    src.pages = (ScalarInts)p.pages + ((int64_t)b * p.max_pages + skip);
+    src.tiles = ntiles;
+    src.last_page = p.n_pages - 1;
+    src.page_elems = (int64_t)p.H_kv * kTileElems;
+    src.head_elems = (int64_t)hk * kTileElems;
+  } else {
+    const int64_t first_row = (int64_t)b * p.NK + (int64_t)skip * kTileRows;
+    src.k = uniform_ptr(p.K + first_row * p.k_stride + hk * kHeadDim);
+    src.v = uniform_ptr(p.V + first_row * p.v_stride + hk * kHeadDim);
+    src.row_bytes = (uint32_t)(p.k_stride * 2);
+    src.v_row_bytes = (uint32_t)(p.v_stride * 2);
+  }
+
+  Wave<kQB, kJ> w;
+  const uint32_t one = c == 0 ? 0x3F803F80u : 0u;
+  w.ones.u = u32x4{one, one, one, one};
+  const uint32_t r_wave = row_begin + wave * kWaveQ;
+#pragma unroll
+  for (int qb = 0; qb < kQB; ++qb)
+#pragma unroll
+    for (int j = 0; j < kJ; ++j) {
+      const RowPlace at = row_place(p, hk, min(r_wave + (qb * kJ + j) * 16 + c, row_end - 1));
+      const uint16_t* q = p.Q + ((int64_t)b * p.NQ + at.q) * p.q_stride + at.head * kHeadDim;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) w.Qf[qb][2 * j + h].u = *reinterpret_cast<const u32x4*>(q + 32 * h + 8 * G);
+    }
+#pragma unroll
+  for (int qb = 0; qb < kQB; ++qb)
+#pragma unroll
+    for (int j = 0; j < kJ; ++j) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const u32x4 raw = w.Qf[qb][2 * j + h].u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          w.Qf[qb][2 * j + h].u[i] = pack_bf16(bf16_lo(raw[i]) * p.scale2, bf16_hi(raw[i]) * p.scale2);
+      }
+      // (General path: zeros that the compiler does not know to be zeros.  Knowing them, it spilled 119 to 326 registers of
+      // the kernels below, in the narrow ones of the fast path too; a build test checks that none does.)
+      float zero = 0.f;
+      if (kGen) asm volatile("" : "+v"(zero));
+      w.mref[qb][j] = zero;
+      w.la[qb][j] = zero;
+      w.L[qb][j] = f32x4{zero, zero, zero, zero};
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt) {
+        f32x4 z = {zero, zero, zero, zero};
+        if (kGen) asm volatile("" : "+v"(z));
+        w.O[qb][j][dt] = z;
+      }
+    }
+  // general path: the reference is the largest of the first 32 keys (agg_attn.hip)
+  auto first_tile = [&]() {
+    if (!kGen) return;
+    const int valid0 = ntiles == 1 ? last_valid : kTileRows;
+#pragma unroll
+    for (int qb = 0; qb < kQB; ++qb) {
+      f32x4 s[2 * kJ];
+      score_unit<kGen, kQB, kJ>(w, qb, s);
+      if (valid0 < 32) mask_unit<kJ>(s, 0, valid0, G);
+#pragma unroll
+      for (int j = 0; j < kJ; ++j) {
+        float mx = s[j][0];
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[kJ * kt + j][r]);
+        mx = quad_max(mx);
+        // a NaN or infinite score cannot serve as reference
+        w.mref[qb][j] = fabsf(mx) < 3.0e38f ? mx : 0.f;
+      }
+    }
+  };
+  const bool done = key_loop<kSrc, kGen, false, kQB, kJ>(w, lds, votes, src, ntiles, last_valid, tid, wave, fa, G, first_tile);
+
+  float l_fin[kQB][kJ];
+  bool unsafe = false;
+#pragma unroll
+  for (int qb = 0; qb < kQB; ++qb)
+#pragma unroll
+    for (int j = 0; j < kJ; ++j) {
+      l_fin[qb][j] = kGen ? quad_sum(w.la[qb][j]) : __shfl(w.L[qb][j][0], c);
+      unsafe = unsafe || !(l_fin[qb][j] < kSumHi) || !(l_fin[qb][j] > kSumLo);
+    }
+  if (!kGen) {
+    if (!done) return false;
+    if (vote(unsafe, votes + kWaves, wave, lane, true)) return false;
+  } else {
+    __syncthreads();  // every wavefront is done with the tiles
+  }
+
+  int here = tid;
+  asm volatile("" : "+v"(here));
+  const int elane = here & 63, ec = here & 15, eG = elane >> 4;
+  if (plan.splits > 1) {
+#pragma unroll
+    for (int qb = 0; qb < kQB; ++qb)
+#pragma unroll
+      for (int j = 0; j < kJ; ++j) {
+        const uint32_t row = r_wave + (qb * kJ + j) * 16 + ec;
+        if (row >= row_end) continue;
+        const int64_t at = partial_row(p, pairs, split, pair, row);
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt) *reinterpret_cast<f32x4*>(p.partial + at * kHeadDim + 16 * dt + 4 * eG) = w.O[qb][j][dt];
+        if (eG == 0)
+          *reinterpret_cast<f32x2*>(partial_sums(p, pairs, plan.splits) + at * 2) =
+              f32x2{kGen ? w.mref[qb][j] : 0.f, l_fin[qb][j]};
+      }
+    return true;
+  }
+  // whole 128-byte rows, turned through a part of the tiles' LDS of the wavefront's own (agg_attn.hip)
+  uint16_t* epi = tiles + wave * (16 * kJ * kEpiStride);
+#pragma unroll
+  for (int qb = 0; qb < kQB; ++qb) {
+    const uint32_t r0 = r_wave + qb * kJ * 16;
+#pragma unroll
+    for (int j = 0; j < kJ; ++j) {
+      const float l = l_fin[qb][j], inv = 1.0f / l;
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt)
+        *reinterpret_cast<u32x2*>(epi + (16 * j + ec) * kEpiStride + 16 * dt + 4 * eG) = pack4(w.O[qb][j][dt] * inv);
+      if (p.lse && eG == 0 && r0 + 16 * j + ec < row_end) {
+        const RowPlace at = row_place(p, hk, r0 + 16 * j + ec);
+        p.lse[((int64_t)b * p.H + at.head) * p.NQ + at.q] = ((kGen ? w.mref[qb][j] : 0.f) + log2f(l)) * kLn2;
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+#pragma unroll
+    for (int i = 0; i < 2 * kJ; ++i) {
+      const uint32_t row = r0 + i * 8 + (elane >> 3);
+      const u32x4 o4 = *reinterpret_cast<const u32x4*>(epi + (i * 8 + (elane >> 3)) * kEpiStride + (elane & 7) * 8);
+      if (row < row_end) {
+        const RowPlace at = row_place(p, hk, row);
+        *reinterpret_cast<u32x4*>(p.O + (((int64_t)b * p.NQ + at.q) * p.H + at.head) * kHeadDim + (elane & 7) * 8) = o4;
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+  }
+  return true;
+}
+
+// The rows of a workgroup that has no keys: zeros, or partial results that add nothing.
+__device__ __forceinline__ void store_nothing(const CrossArgs& p, const CrossPlan& plan, int64_t pairs, int64_t pair, int split,
+                                              uint32_t row_begin, uint32_t row_end, bool no_keys) {
+  const int b = (int)(pair / p.H_kv), hk = (int)(pair % p.H_kv), quad = threadIdx.x & 15;
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  for (uint32_t row = row_begin + (threadIdx.x >> 4); row < row_end; row += kAttnThreads / 16) {
+    if (plan.splits == 1) {
+      store_row(p, b, hk, row, quad, 0.f, 0.f, zero, no_keys);
+      continue;
+    }
+    const int64_t at = partial_row(p, pairs, split, pair, row);
+    *reinterpret_cast<f32x4*>(p.partial + at * kHeadDim + 4 * quad) = zero;
+    if (quad == 0) *reinterpret_cast<f32x2*>(partial_sums(p, pairs, plan.splits) + at * 2) = f32x2{-INFINITY, 0.f};
+  }
+}
+
+}  // namespace
+
+struct WideArgs {
+  CrossArgs a;
+  CrossPlan plan;
+};
+
+// The kernel's arguments again, so that what one path derives from them is not held for another (agg_attn.hip).
+__device__ __forceinline__ const WideArgs& wide_args_again() {
+  typedef const __attribute__((address_space(4))) WideArgs* KernelArgs;
+  KernelArgs args = (KernelArgs)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(args));
+  return *(const WideArgs*)args;
+}
+
+template <int kSrc, int kTail>
+__global__ __launch_bounds__(kAttnThreads, kBlocksPerCu) void cross_wide_kernel(WideArgs w) {
+  __shared__ __align__(16) uint16_t tiles[2 * kLdsTiles * kTileElems];
+  __shared__ __align__(16) uint32_t votes[kVoteWords];
+  const CrossArgs& a = w.a;
+  const int npairs = a.B * a.H_kv;
+  // the workgroups of a pair's split read the same keys: on one XCD they share them through its L2
+  int unit, i;
+  if (!list_tile(tile_list(npairs * w.plan.splits, (int)w.plan.row_tiles), npairs * w.plan.splits, blockIdx.x, unit, i)) return;
+  const int pair = unit % npairs, split = unit / npairs, b = pair / a.H_kv;
+  const uint32_t rows = (uint32_t)cross_queries(a, b) * (uint32_t)a.group;
+  const uint32_t row_begin = (uint32_t)i * (uint32_t)w.plan.width;
+  if (row_begin >= rows) return;
+  const uint32_t row_end = min(rows, row_begin + (uint32_t)w.plan.width);
+  const int n = cross_keys(a, b);
+  const int64_t all = ((int64_t)n + kTileRows - 1) / kTileRows;
+  if (all * split / w.plan.splits == all * (split + 1) / w.plan.splits) {
+    store_nothing(a, w.plan, npairs, pair, split, row_begin, row_end, n == 0);
+    return;
+  }
+  bool done;
+  if (kTail != 0 && row_end - row_begin <= kTail)
+    done = attend_cross<kSrc, false, kTail == 192 ? 3 : 2, 1>(a, w.plan, npairs, tiles, votes, pair, split, row_begin, row_end);
+  else
+    done = attend_cross<kSrc, false, 2, 2>(a, w.plan, npairs, tiles, votes, pair, split, row_begin, row_end);
+  if (done) return;
+  const WideArgs& again = wide_args_again();
+#pragma unroll 1
+  for (uint32_t r = row_begin; r < row_end; r += kWaves * wave_queries(2, 1)) {
+    __syncthreads();  // the LDS is free
+    attend_cross<kSrc, true, 2, 1>(again.a, again.plan, npairs, tiles, votes, pair, split, r,
+                                   min(row_end, r + (uint32_t)(kWaves * wave_queries(2, 1))));
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Joins the splits' results: sixteen threads a row and group, kGroups groups a row, each with every kGroups-th split.  Bound by the
+// partial results' bytes where there are many rows, by one read's latency where there are few: four splits are requested
+// before one is used, and the groups meet in LDS.
+// ---------------------------------------------------------------------------
 constexpr int kJoinThreads = 256;
+constexpr int join_rows(int groups) { return kJoinThreads / 16 / groups; }
+
+template <int kGroups>
 __global__ __launch_bounds__(kJoinThreads) void cross_join_kernel(CrossArgs a, int splits, int64_t pairs, int64_t first) {
+  __shared__ __align__(16) float meet[kJoinThreads / 16][kRowFloats];
   const int64_t all = (int64_t)a.NQ * a.group;
-  const int64_t at = first + (int64_t)blockIdx.x * (kJoinThreads / 16) + (threadIdx.x >> 4);
-  const int quad = threadIdx.x & 15;
-  if (at >= pairs * all) return;
-  const int64_t pair = at / all;
+  const int slot = threadIdx.x >> 4, quad = threadIdx.x & 15, group = slot % kGroups;
+  const int64_t at = first + (int64_t)blockIdx.x * join_rows(kGroups) + slot / kGroups;
+  const int64_t pair = min(at, pairs * all - 1) / all;
   const uint32_t row = (uint32_t)(at - pair * all);
   const int b = (int)(pair / a.H_kv), hk = (int)(pair % a.H_kv);
-  if (row >= (uint32_t)cross_queries(a, b) * (uint32_t)a.group) return;
-  const f32x2* const sums = reinterpret_cast<const f32x2*>(a.partial + (int64_t)splits * pairs * all * kHeadDim);
-  float top = -INFINITY;
-  for (int s = 0; s < splits; ++s) top = fmaxf(top, sums[at + (int64_t)s * pairs * all][0]);
-  const float ref = top == -INFINITY ? 0.f : top;
-  float total = 0.f;
+  const int n = a.k_lens ? min(max(a.k_lens[b], 0), a.NK) : a.NK;
+  const int queries = a.q_lens ? min(max(a.q_lens[b], 0), a.NQ) : a.NQ;
+  const bool here = at < pairs * all && row < (uint32_t)queries * (uint32_t)a.group;
+  float m = -INFINITY, l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < splits; ++s) {
-    const int64_t p = at + (int64_t)s * pairs * all;
-    const f32x2 x = sums[p];
-    const float f = fast_exp2(x[0] - ref);  // 0 for a split without keys
-    total += x[1] * f;
-    o += *reinterpret_cast<const f32x4*>(a.partial + p * kHeadDim + 4 * quad) * f;
+  // another part of the sum, by its reference (-infinity: a split without keys, which adds nothing)
+  auto add = [&](float m2, float l2, f32x4 o2) {
+    const float now = fmaxf(m, m2), ref = now == -INFINITY ? 0.f : now;
+    const float f = fast_exp2(m - ref), f2 = fast_exp2(m2 - ref);
+    m = now;
+    l = l * f + l2 * f2;
+    o = o * f + o2 * f2;
+  };
+  if (here) {
+    const f32x2* const sums = reinterpret_cast<const f32x2*>(partial_sums(a, pairs, splits)) + at;
+    const float* const from = a.partial + at * kHeadDim + 4 * quad;
+    const int64_t next = pairs * all;
+    for (int s0 = group; s0 < splits; s0 += 4 * kGroups) {
+      f32x2 x[4];
+      f32x4 part[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int s = min(s0 + i * kGroups, splits - 1);
+        x[i] = sums[s * next];
+        part[i] = *reinterpret_cast<const f32x4*>(from + s * next * kHeadDim);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (s0 + i * kGroups < splits) add(x[i][0], x[i][1], part[i]);
+    }
   }
-  store_row(a, b, hk, row, quad, ref, total, o, cross_keys(a, b) == 0);
+  if constexpr (kGroups > 1) {
+    *reinterpret_cast<f32x4*>(&meet[slot][4 * quad]) = o;
+    if (quad == 0) *reinterpret_cast<f32x2*>(&meet[slot][kHeadDim]) = f32x2{m, l};
+    __syncthreads();
+    if (group) return;
+#pragma unroll 4
+    for (int g = 1; g < kGroups; ++g) {
+      const f32x2 x = *reinterpret_cast<const f32x2*>(&meet[slot + g][kHeadDim]);
+      add(x[0], x[1], *reinterpret_cast<const f32x4*>(&meet[slot + g][4 * quad]));
+    }
+  }
+  if (here) store_row(a, b, hk, row, quad, m == -INFINITY ? 0.f : m, l, o, n == 0);
 }
+
+template <int kGroups>
+static void launch_join(const CrossArgs& a, int splits, int64_t pairs, int64_t rows, hipStream_t st) {
+  constexpr int64_t kRows = join_rows(kGroups), kMost = kRows << 22;
+  for (int64_t first = 0; first < pairs * rows; first += kMost) {
+    const int64_t here = pairs * rows - first < kMost ? pairs * rows - first : kMost;
+    hipLaunchKernelGGL(cross_join_kernel<kGroups>, dim3((unsigned)((here + kRows - 1) / kRows)), dim3(kJoinThreads), 0, st, a,
+                       splits, pairs, first);
+  }
+}
+
+// the wide kernel reaches a tile's 64 rows with 32-bit byte offsets
+static bool wide_fits(int64_t stride) { return stride <= ((int64_t)1 << 23); }
 
 size_t cross_partial_floats(int64_t B, int64_t NQ, int64_t NK, int64_t H, int64_t H_kv) {
   const int64_t pairs = B * H_kv, rows = NQ * (H / H_kv);
-  const CrossPlan p = plan_cross(pairs, rows, NK);
-  return p.splits > 1 ? (size_t)p.splits * pairs * rows * (kHeadDim + 2) : 0;
+  // a call's strides choose between two plans: enough for either
+  const int a = plan_cross(pairs, rows, NK, true).splits, b = plan_cross(pairs, rows, NK, false).splits, splits = a > b ? a : b;
+  return splits > 1 ? (size_t)splits * pairs * rows * (kHeadDim + 2) : 0;
 }
 
 template <bool kPaged>
@@ -298,25 +583,58 @@ static void launch_few(const CrossArgs& a, const CrossPlan& p, int64_t pairs, hi
   constexpr int64_t kMost = 1 << 22;  // workgroups of a launch (kLaunchRows)
   for (int64_t first = 0; first < groups; first += kMost) {
     const dim3 grid((unsigned)(groups - first < kMost ? groups - first : kMost));
-    if (p.tiles == 1) hipLaunchKernelGGL((cross_few_kernel<kPaged, 1>), grid, dim3(few_threads(1)), 0, st, a, p, pairs, first);
-    else if (p.tiles == 2) hipLaunchKernelGGL((cross_few_kernel<kPaged, 2>), grid, dim3(few_threads(2)), 0, st, a, p, pairs, first);
-    else hipLaunchKernelGGL((cross_few_kernel<kPaged, 4>), grid, dim3(few_threads(4)), 0, st, a, p, pairs, first);
+    if (p.tiles == 1) hipLaunchKernelGGL((cross_few_kernel<kPaged, 1>), grid, dim3(kFewThreads), 0, st, a, p, pairs, first);
+    else hipLaunchKernelGGL((cross_few_kernel<kPaged, 2>), grid, dim3(kFewThreads), 0, st, a, p, pairs, first);
   }
+}
+
+template <int kSrc>
+static hipError_t launch_wide(const CrossArgs& a, const CrossPlan& p, hipStream_t st) {
+  // workgroups of a launch (kLaunchRows): beyond that parts of the batch are launches of their own, which share out nothing along the keys
+  constexpr int64_t kMost = 1 << 22;
+  const int64_t of_one = (int64_t)a.H_kv * p.row_tiles * p.splits;
+  if (of_one > kMost) return hipErrorInvalidConfiguration;
+  const int64_t step = a.B * of_one <= kMost ? a.B : kMost / of_one;
+  if (step < a.B && p.splits > 1) return hipErrorInvalidConfiguration;
+  for (int64_t b = 0; b < a.B; b += step) {
+    WideArgs w = {a, p};
+    w.a.B = (int32_t)(a.B - b < step ? a.B - b : step);
+    w.a.Q += b * a.NQ * a.q_stride;
+    w.a.O += b * a.NQ * a.H * kHeadDim;
+    if (a.lse) w.a.lse += b * a.H * a.NQ;
+    if (kSrc == kSrcPaged) {
+      w.a.pages += b * a.max_pages;
+    } else if (a.NK > 0) {
+      w.a.K += b * a.NK * a.k_stride;
+      w.a.V += b * a.NK * a.v_stride;
+    }
+    if (a.q_lens) w.a.q_lens += b;
+    if (a.k_lens) w.a.k_lens += b;
+    const dim3 grid((unsigned)tile_list((int)(w.a.B * a.H_kv * p.splits), (int)p.row_tiles).groups);
+    const dim3 block(kAttnThreads);
+    const int narrow = p.width == 128 ? 128 : p.tail;
+    if (narrow == 0) hipLaunchKernelGGL((cross_wide_kernel<kSrc, 0>), grid, block, 0, st, w);
+    else if (narrow == 192) hipLaunchKernelGGL((cross_wide_kernel<kSrc, 192>), grid, block, 0, st, w);
+    else hipLaunchKernelGGL((cross_wide_kernel<kSrc, 128>), grid, block, 0, st, w);
+  }
+  return hipSuccess;
 }
 
 hipError_t launch_cross(const CrossArgs& a, hipStream_t st) {
   const int64_t pairs = (int64_t)a.B * a.H_kv, rows = (int64_t)a.NQ * a.group;
-  const CrossPlan p = plan_cross(pairs, rows, a.NK);
+  const CrossPlan p = plan_cross(pairs, rows, a.NK, a.pages || (wide_fits(a.k_stride) && wide_fits(a.v_stride)));
   (void)hipGetLastError();
-  if (a.pages) launch_few<true>(a, p, pairs, st);
-  else launch_few<false>(a, p, pairs, st);
+  if (p.wide) {
+    const hipError_t e = a.pages ? launch_wide<kSrcPaged>(a, p, st) : launch_wide<kSrcStrided>(a, p, st);
+    if (e != hipSuccess) return e;
+  } else if (a.pages) {
+    launch_few<true>(a, p, pairs, st);
+  } else {
+    launch_few<false>(a, p, pairs, st);
+  }
   if (p.splits > 1) {
-    constexpr int64_t kRows = kJoinThreads / 16, kMost = kRows << 22;
-    for (int64_t first = 0; first < pairs * rows; first += kMost) {
-      const int64_t here = pairs * rows - first < kMost ? pairs * rows - first : kMost;
-      hipLaunchKernelGGL(cross_join_kernel, dim3((unsigned)((here + kRows - 1) / kRows)), dim3(kJoinThreads), 0, st, a, p.splits,
-                         pairs, first);
-    }
+    if (pairs * rows <= 4096 && p.splits > 4) launch_join<16>(a, p.splits, pairs, rows, st);
+    else launch_join<1>(a, p.splits, pairs, rows, st);
   }
   return hipGetLastError();
 }

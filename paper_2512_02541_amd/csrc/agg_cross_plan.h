@@ -8,24 +8,73 @@ namespace agg {
 
 // A pair is a (batch element, key head); its rows are its queries by the heads that share the key head.
 struct CrossPlan {
-  int tiles;          // 16-row tiles of a wavefront
+  int wide;           // the kernel of many rows (cross_wide_kernel), else that of few (cross_few_kernel)
+  int tiles;          // few: 16-row tiles of a wavefront
+  int width;          // wide: rows of a workgroup, 256 or 128
+  int tail;           // wide: rows of a pair's last workgroup where they are fewer, 0: it is as wide as the others
   int64_t row_tiles;  // workgroups along a pair's rows
   int splits;         // ... along its keys; more than one: partial results, joined by a second launch
 };
 
-constexpr int kFewWaves = 8;   // wavefronts of a workgroup, each with keys of its own (four of 64 rows)
-constexpr int kKeyBlock = 32;  // keys of a wavefront's step
+constexpr int kFewWaves = 8;    // wavefronts of a workgroup, each with keys of its own
+constexpr int kKeyBlock = 32;   // keys of a wavefront's step
+constexpr int kFewRows = 32;    // most rows of such a workgroup
+constexpr int kWideRows = 256;  // rows of a wide workgroup
+constexpr int kMostSplits = 64;
+constexpr int kMostShared = 4096;  // most workgroups of a call that is shared out along the keys
 
-inline int few_waves(int tiles) { return tiles == 4 ? 4 : kFewWaves; }
-
-inline CrossPlan plan_cross(int64_t pairs, int64_t rows, int64_t keys) {
+// wide_fits: the distances between rows are what the wide kernel can address
+inline CrossPlan plan_cross(int64_t pairs, int64_t rows, int64_t keys, bool wide_fits) {
   CrossPlan p;
-  p.tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  p.width = p.tail = 0;
+  p.tiles = rows <= 16 ? 1 : 2;
   p.row_tiles = (rows + 16 * p.tiles - 1) / (16 * p.tiles);
-  const int64_t groups = pairs * p.row_tiles, steps = (keys + kKeyBlock - 1) / kKeyBlock / few_waves(p.tiles);
-  int64_t splits = 512 / (groups < 1 ? 1 : groups);
-  if (splits > steps / 2) splits = steps / 2;
-  p.splits = splits < 1 ? 1 : (int)splits;
+  // Up to 32 rows the kernel of few rows.  Up to 64 while its two workgroups of a pair all run at once: us, few / wide, paged, 16 heads, 64 queries
+  // to 262 keys 5.4 / 6.7, to 5496 12.6 / 19.4, to 137400 106 / 105; with 384 pairs to 1374 keys 45.7 / 26.1.
+  p.wide = wide_fits && rows > kFewRows && (rows > 2 * kFewRows || pairs * p.row_tiles > 256);
+  if (!p.wide) {
+    // Splits by predicted time: a start, a wavefront's steps one after another, and a second launch.  More workgroups than run at once
+    // (two on a CU of up to 16 rows, one of more) gain nothing: the memory is busy with them.
+    const int64_t groups = pairs * p.row_tiles, steps = (keys + kKeyBlock * kFewWaves - 1) / (kKeyBlock * kFewWaves);
+    const int64_t at_once = p.tiles == 1 ? 512 : 256;
+    const double step = p.tiles == 1 ? 0.55 : 0.85;
+    double best = 0;
+    p.splits = 1;
+    for (int64_t s = 1; s <= kMostSplits && (s == 1 || (groups * s <= at_once && steps / s >= 1)); ++s) {
+      const double us = (double)((steps + s - 1) / s) * step + (s > 1 ? 3.0 + 0.03 * s : 0.0);
+      if (s == 1 || us < best) {
+        best = us;
+        p.splits = (int)s;
+      }
+    }
+    return p;
+  }
+  // Width and splits by predicted time: rounds of 512 workgroups (two on a CU; alone on it one takes little more than half as
+  // long), each with its start, its end and its share of the key tiles; a second launch and the partial results' way to
+  // memory and back.
+  const int64_t tiles = (keys + 63) / 64;
+  double best = -1;
+  p.width = p.splits = 0;
+  for (int width = kWideRows; width >= 128; width -= 128) {
+    const int64_t row_tiles = (rows + width - 1) / width;
+    const int rest = (int)(rows % width);
+    const int tail = width == 128 || rest == 0 ? 0 : rest <= 128 ? 128 : rest <= 192 ? 192 : 0;
+    const double pair = width == 128 ? 0.565 : 1.0, alone = width == 128 ? 0.34 : 0.535;
+    const double saved = tail ? (tail == 128 ? 0.435 : 0.21) / (double)row_tiles : 0.0;  // by narrow last workgroups
+    for (int s = 1; s <= kMostSplits && (s == 1 || (tiles / s >= 4 && pairs * row_tiles * s <= kMostShared)); ++s) {
+      const int64_t groups = pairs * row_tiles * s, rest_groups = groups % 512;
+      const double rounds = (double)(groups / 512) * pair + (rest_groups == 0 ? 0.0 : rest_groups <= 256 ? alone : pair);
+      double us = rounds * (groups > 512 ? 1.0 - saved : 1.0) * (5.0 + 1.65 * (double)((tiles + s - 1) / s));
+      if (s > 1) us += 4.0 + (double)pairs * (double)rows * s * 66 * 8 / 4.4e6;
+      if (best < 0 || us < best) {
+        best = us;
+        p.width = width;
+        p.tail = tail;
+        p.row_tiles = row_tiles;
+        p.splits = s;
+      }
+    }
+  }
   return p;
 }
 

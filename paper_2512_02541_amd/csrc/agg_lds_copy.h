@@ -9,6 +9,8 @@
 namespace agg {
 
 typedef __attribute__((address_space(3))) char lds_char;
+// numbers that a launch only reads, at places that all lanes agree on: read by the scalar unit
+typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
 
 // Workgroup barrier that orders LDS traffic only: global loads issued for a later tile
 // stay in flight across it.

@@ -1,5 +1,7 @@
 """Attention to keys of another length and the paged cache without a GPU: the oracle's pins, sizes, refusals and the
 launch plan."""
+import os
+import re
 import subprocess
 
 import pytest
@@ -201,9 +203,10 @@ DRIVER = r"""
 #include "agg_cross_plan.h"
 int main() {
   long long pairs, rows, keys;
-  while (scanf("%lld %lld %lld", &pairs, &rows, &keys) == 3) {
-    const agg::CrossPlan p = agg::plan_cross(pairs, rows, keys);
-    printf("%d %lld %d\n", p.tiles, (long long)p.row_tiles, p.splits);
+  int fits;
+  while (scanf("%lld %lld %lld %d", &pairs, &rows, &keys, &fits) == 4) {
+    const agg::CrossPlan p = agg::plan_cross(pairs, rows, keys, fits);
+    printf("%d %d %lld %d\n", p.wide ? p.width / 16 : p.tiles, p.tail, (long long)p.row_tiles, p.splits);
   }
 }
 """
@@ -217,7 +220,7 @@ def plan(tmp_path_factory):
                            "-o", str(d / "plan"), str(d / "plan.cpp")])
 
     def ask(sizes):
-        text = "".join("%d %d %d\n" % s for s in sizes)
+        text = "".join("%d %d %d %d\n" % s for s in sizes)
         out = subprocess.run([str(d / "plan")], input=text, text=True, check=True, stdout=subprocess.PIPE).stdout
         return [tuple(int(x) for x in line.split()) for line in out.splitlines()]
 
@@ -225,8 +228,59 @@ def plan(tmp_path_factory):
 
 
 def test_every_row_has_a_workgroup_and_every_split_keys(plan):
-    sizes = [(pairs, rows, keys) for pairs in (1, 3, 16, 100, 4096, 2 ** 31 - 1) for rows in (1, 16, 17, 33, 64, 65, 257, 1374, 10992, 2 ** 30)
-             for keys in (0, 1, 31, 64, 1000, 20000, 137400, 2 ** 31 - 600)]
-    for (pairs, rows, keys), (tiles, row_tiles, splits) in zip(sizes, plan(sizes)):
+    sizes = [(pairs, rows, keys, fits) for pairs in (1, 3, 16, 100, 4096, 2 ** 31 - 1)
+             for rows in (1, 16, 17, 33, 64, 65, 257, 400, 1374, 10992, 2 ** 30)
+             for keys in (0, 1, 31, 64, 1000, 20000, 137400, 2 ** 31 - 600) for fits in (0, 1)]
+    for (pairs, rows, keys, fits), (tiles, tail, row_tiles, splits) in zip(sizes, plan(sizes)):
         assert row_tiles * 16 * tiles >= rows > (row_tiles - 1) * 16 * tiles
-        assert 1 <= splits <= max(1, keys // 32)
+        assert tiles in (1, 2, 8, 16) and (fits or tiles < 8)
+        assert (tiles >= 8) == (fits and rows > 64 or fits and rows > 32 and pairs * 2 > 256)
+        assert tail in (0, 128, 192) and (tail == 0 or (tiles == 16 and 0 < rows % 256 <= tail))
+        assert 1 <= splits <= max(1, keys // 32) and splits <= 512
+
+
+def test_parts_of_a_batch_share_out_no_keys(plan):
+    """More workgroups than a launch takes: no splits, whose partial results a launch of its own could not find."""
+    sizes = [(pairs, rows, 2 ** 31 - 600, 1) for pairs in (2 ** 22, 2 ** 23 + 5, 2 ** 31 - 1) for rows in (65, 256, 1000)]
+    assert all(splits == 1 for _, _, _, splits in plan(sizes))
+
+
+# ---- the code that is built ----------------------------------------------------------------------------
+@pytest.fixture(scope="module")
+def assembly(tmp_path_factory):
+    out = tmp_path_factory.mktemp("asm") / "agg_cross.s"
+    subprocess.check_call([b.HIPCC, *b.FLAGS, "-I", os.path.join(b.ROOT, "include"), "-I", b.CSRC, "-S", "--cuda-device-only",
+                           os.path.join(b.CSRC, "agg_cross.hip"), "-o", str(out)], stderr=subprocess.DEVNULL)
+    return out.read_text()
+
+
+def test_kernels_leave_m0_to_their_copy_statements(assembly):
+    """The copies into LDS set M0 inside assembly statements without declaring it (the compiler rejects it as a clobber),
+    which is sound only while no instruction of the compiler's uses it."""
+    inside, seen_copy, offenders = False, 0, []
+    for line in assembly.splitlines():
+        code = line.split(";")[0] if not line.lstrip().startswith(";;#") else line
+        if "#ASMSTART" in line:
+            inside = True
+        elif "#ASMEND" in line:
+            inside = False
+        elif inside:
+            seen_copy += "global_load_lds_dwordx4" in code
+        elif re.search(r"\bm0\b", code):
+            offenders.append(line.strip())
+    assert seen_copy >= 4, "the copy statements were not found"
+    assert not offenders, offenders[:5]
+
+
+def test_kernels_do_not_spill(assembly):
+    """The wide kernels hold two paths' code: nothing of the second may lie in scratch memory while the first runs."""
+    seen, spilled = 0, []
+    for kernel in re.split(r"^  - \.", assembly, flags=re.M):
+        name = re.search(r"\.name: +\S*(cross_\w+_kernel\S*)", kernel)
+        if name:
+            seen += 1
+            field = {f: int(re.search(r"\.%s: +(\d+)" % f, kernel).group(1))
+                     for f in ("vgpr_spill_count", "private_segment_fixed_size")}
+            if any(field.values()):
+                spilled.append((name.group(1), field))
+    assert seen >= 12 and not spilled, spilled

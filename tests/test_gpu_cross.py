@@ -6,7 +6,7 @@ Tolerances count roundings.  With A the sum of probability times |v| of a row's 
        rounded or the unrounded ones: 2 * 2^-8 A.  The result is rounded to bf16: 2^-8 |O|.  Logits are sums of 64 exact
        products in float32, 2^-24 of S each, and every other float32 step (exponential, scale, sums of up to
        2^18 keys in lanes and blocks) is under 2^-14 together: 2^-12 (A + S A).
-       Up to 64 rows a key head (queries by heads that share it) that is all.  Beyond, scale*log2(e)*Q is rounded to
+       Up to 32 rows a key head (queries by heads that share it) that is all.  Beyond, scale*log2(e)*Q is rounded to
        bf16 first: a logit moves by up to d = 2^-8 S, a probability by the factor e^(2 d): (e^(2 d) - 1) A more.
   lse  2^-18 S + 2^-16 (1 + |lse|) for the first; beyond, d and 2^-7 more for rounded probabilities.
 """
@@ -24,7 +24,7 @@ from paper_2512_02541_amd import harness
 pytestmark = pytest.mark.gpu
 
 HALF = 2.0 ** -8
-FEW = 64
+FEW = 32
 
 
 def say(*a):
