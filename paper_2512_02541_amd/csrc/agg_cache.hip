@@ -10,69 +10,106 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 // ---------------------------------------------------------------------------
-// A workgroup takes 32 consecutive rows: half a page of a sequence (keys and values) or 32 tokens (queries).  It works out
-// their cosines and signed sines once, a pair of channels a thread, and its wavefronts take the heads in turn, eight lanes a
-// row of a head.  A key's 16-byte chunk goes to the page from the registers it was turned in: eight consecutive rows make a
-// whole 128-byte line of one chunk number.  Values turn through LDS with the transposing read, which leaves a lane with
-// the eight rows of one channel that make a chunk of the page; a chunk that the new rows fill only in part is
-// stored element by element, so that its other rows stay.
+// A workgroup takes 32 consecutive rows of a sequence, half a page, and the tokens that become them: keys, values and queries.
+// It works out their cosines and signed sines once, a pair of channels a thread, and its wavefronts take the heads in turn, eight
+// lanes a row of a head, a head's rows requested while the one before is worked on.  A key's 16-byte chunk goes to the page
+// from the registers it was turned in: eight consecutive rows make a whole 128-byte line of one chunk number.  Values turn
+// through LDS with the transposing read, which leaves a lane with the eight rows of one channel that make a chunk of the
+// page; a chunk that the new rows fill only in part is stored element by element, so that its other rows stay.
 // ---------------------------------------------------------------------------
 constexpr int kAppendThreads = 256;
 constexpr int kAppendWaves = kAppendThreads / 64;
 constexpr int kAppendRows = 32;
-constexpr int kHeadStride = kHeadDim + 4;  // floats of a head in LDS: 16-byte aligned rows
 
 namespace {
 
+// Where a channel's partner is: nowhere (nothing turns), beside it in the same lane's registers, in another lane's register of the
+// same number, or anywhere.
+enum { kNoPairs, kPairsInLane, kPairsAcrossLanes, kPairsAnywhere };
+
 // What a lane knows of its eight channels of any row.
 struct Channels {
-  int other[8];     // each channel's other one
-  uint32_t turned;  // whether it turns at all
-  float gamma[8], beta[8];
-  int kind;
-  float eps;
+  uint32_t other[2];    // a byte each: the channel's other one, bit 7: it turns at all
+  int lane_at;          // kPairsAcrossLanes: 4 * the lane that holds the others
 };
 
-// norm and rotation of a row's eight channels; head: floats of this group of eight lanes, turns: the row's table
-__device__ __forceinline__ void turn8(float (&x)[8], const Channels& ch, bool turns_any, int c0, float* head, const f32x2* turns) {
-  if (ch.kind != AGG_NORM_NONE) {
-    float mean = 0.f;
-    if (ch.kind == AGG_NORM_LAYER) {
+// orders this wavefront's LDS writes before its later reads, and its earlier reads before its later writes
+// (wave_lds_fence); a row's table of cosines and signed sines: 16-byte chunk q of lane j (channels 8 j + 2 q, + 1) at this place,
+// so that the sixteen lanes served together, of two rows, read from different banks
+__device__ __forceinline__ int turn_chunk(int row, int q, int j) { return row * 32 + ((q * 8 + j) ^ (8 * (row & 1))); }
+
+// norm of a row's eight channels.  affine: what the norm multiplies by (from the lane's first channel on) and, kHeadDim behind, adds
+__device__ __forceinline__ void norm8(float (&x)[8], int kind, float eps, const float* affine) {
+  float mean = 0.f;
+  if (kind == AGG_NORM_LAYER) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) mean += x[i];
-      mean = sum_of_8(mean) * (1.f / kHeadDim);
-    }
-    float sq = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      x[i] -= mean;
-      sq += x[i] * x[i];
-    }
-    const float r = rsqrtf(sum_of_8(sq) * (1.f / kHeadDim) + ch.eps);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = x[i] * r * ch.gamma[i] + ch.beta[i];
+    for (int i = 0; i < 8; ++i) mean += x[i];
+    mean = sum_of_8(mean) * (1.f / kHeadDim);
   }
-  if (!turns_any) return;
-  wave_lds_fence();
-  *reinterpret_cast<f32x4*>(head + c0) = f32x4{x[0], x[1], x[2], x[3]};
-  *reinterpret_cast<f32x4*>(head + c0 + 4) = f32x4{x[4], x[5], x[6], x[7]};
-  wave_lds_fence();
-  f32x4 cs[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) cs[i] = *reinterpret_cast<const f32x4*>(turns + c0 + 2 * i);
+  float sq = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float y = x[i] * cs[i / 2][i % 2 * 2] + head[ch.other[i]] * cs[i / 2][i % 2 * 2 + 1];
-    x[i] = (ch.turned >> i) & 1 ? y : x[i];  // by selection: an infinity times 0 is none of the other channels' business
+    x[i] -= mean;
+    sq += x[i] * x[i];
   }
+  const float r = rsqrtf(sum_of_8(sq) * (1.f / kHeadDim) + eps);
+#pragma unroll
+  for (int i = 0; i < 8; i += 4) {
+    const f32x4 g = *reinterpret_cast<const f32x4*>(affine + i);
+    const f32x4 b = *reinterpret_cast<const f32x4*>(affine + kHeadDim + i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[i + e] = x[i + e] * r * g[e] + b[e];
+  }
+}
+
+// rotation of a row's eight channels; scratch: 512 floats of this wavefront
+template <int kPairs>
+__device__ __forceinline__ void turn8(float (&x)[8], const Channels& ch, int lane, int row, const f32x4* turns, float* scratch) {
+  if constexpr (kPairs == kNoPairs) return;
+  const int j = lane & 7;
+  float y[8];
+  if constexpr (kPairs == kPairsInLane) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = x[i ^ 1];
+  } else if constexpr (kPairs == kPairsAcrossLanes) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = __int_as_float(__builtin_amdgcn_ds_bpermute(ch.lane_at, __float_as_int(x[i])));
+  } else {
+    // register i of all lanes in a row of 64 floats: every access of a lane group falls on as many banks as it has lanes, save where
+    // a section ends inside a lane
+    wave_lds_fence();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) scratch[i * 64 + lane] = x[i];
+    wave_lds_fence();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t other = ch.other[i / 4] >> (8 * (i % 4));
+      y[i] = scratch[(other & 7u) * 64 + (lane & 56) + ((other >> 3) & 7u)];
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const f32x4 cs = turns[turn_chunk(row, q, j)];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int i = 2 * q + e;
+      const float turned = x[i] * cs[2 * e] + y[i] * cs[2 * e + 1];
+      // by selection: an infinity times 0 is none of the other channels' business
+      y[i] = (ch.other[i / 4] >> (8 * (i % 4))) & 0x80u ? turned : x[i];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = y[i];
 }
 
 }  // namespace
 
+template <int kPairs>
 __global__ __launch_bounds__(kAppendThreads, 3) void append_kernel(AppendArgs a) {
-  __shared__ __align__(16) f32x2 turns[kAppendRows][kHeadDim];
-  __shared__ __align__(16) float heads[kAppendWaves][8][kHeadStride];
-  __shared__ __align__(16) uint16_t values[kAppendWaves][kAppendRows * kHeadDim];
+  __shared__ __align__(16) f32x4 turns[kAppendRows * 32];
+  // of a wavefront: eight rows of a head while they are turned, then a head's values while they are transposed
+  __shared__ __align__(16) uint16_t space[kAppendWaves][kAppendRows * kHeadDim];
+  __shared__ __align__(16) float affine[2][2 * kHeadDim];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row8 = lane >> 3, j = lane & 7, c0 = j * 8;  // this lane's row of eight, chunk of a head, first channel
@@ -81,74 +118,73 @@ __global__ __launch_bounds__(kAppendThreads, 3) void append_kernel(AppendArgs a)
 
   Channels ch;
   const uint64_t others = *reinterpret_cast<const uint64_t*>(r.other + c0);
-  ch.turned = 0;
+  ch.other[0] = (uint32_t)others;
+  ch.other[1] = (uint32_t)(others >> 32);
+  ch.lane_at = ((lane & 56) + (int)((others >> 3) & 7)) * 4;
+  if (threadIdx.x < 2 * kHeadDim) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    ch.other[i] = (int)(others >> (8 * i)) & 63;
-    if ((others >> (8 * i)) & 0x80) ch.turned |= 1u << i;
+    for (int t = 0; t < 2; ++t) {
+      const float* const of = threadIdx.x < kHeadDim ? r.norm[t].gamma : r.norm[t].beta;
+      affine[t][threadIdx.x] = of ? of[threadIdx.x % kHeadDim] : threadIdx.x < kHeadDim ? 1.f : 0.f;
+    }
   }
-  // this thread's pair of every eighth row's
-  const int p = threadIdx.x % (kHeadDim / 2);
-  const int axis = r.axis[p], lo = r.first[p], hi = r.second[p];
-  const uint64_t freq = r.freq[p];
-  float* const head = heads[wave][row8];
-  if (r.pairs && r.pairs < kHeadDim / 2)  // channels that no pair writes
-    for (int i = threadIdx.x; i < kAppendRows * kHeadDim; i += kAppendThreads)
-      if (!(r.other[i % kHeadDim] & 0x80)) turns[i / kHeadDim][i % kHeadDim] = f32x2{1.f, 0.f};
+  // channel c's cosine and signed sine in a row's table
+  f32x2* const table = reinterpret_cast<f32x2*>(turns);
+  auto table_at = [](int row, int c) { return turn_chunk(row, (c & 7) >> 1, c >> 3) * 2 + (c & 1); };
 
-  for (int64_t item = blockIdx.x; item < a.k_items + a.q_items; item += gridDim.x) {
-    const bool keys = item < a.k_items;
-    const uint32_t it = (uint32_t)(keys ? item : item - a.k_items);  // fewer than 2^32 of either (launch_append)
-    const uint32_t parts = keys ? a.k_parts : a.q_parts, units = keys ? a.k_units : a.q_units;
-    const int part = (int)(it % parts), unit = (int)(it / parts % units), b = (int)(it / parts / units);
-    // rows of the unit: key rows of the cache, which are tokens from start on; or tokens
-    const int64_t start = keys && a.start ? ((ScalarInts)a.start)[b] : 0;
+  for (int64_t item = blockIdx.x; item < a.items; item += gridDim.x) {
+    const uint32_t it = (uint32_t)item;  // fewer than 2^32 (launch_append)
+    const int part = (int)(it % (uint32_t)a.parts), unit = (int)(it / (uint32_t)a.parts % (uint32_t)a.units),
+              b = (int)(it / (uint32_t)a.parts / (uint32_t)a.units);
+    const int64_t start = a.start ? ((ScalarInts)a.start)[b] : 0;
     const int count = a.counts ? min(max(((ScalarInts)a.counts)[b], 0), T) : T;
     const int64_t cap = (int64_t)a.max_pages * kTileRows;
-    const int64_t row0 = (keys ? max(start, (int64_t)0) / kAppendRows : 0) * kAppendRows + (int64_t)unit * kAppendRows;
-    const int64_t tok0 = row0 - start;  // the unit's first row is this token
-    if (keys && unit == 0 && part == 0 && threadIdx.x == 0 && a.lens)
-      a.lens[b] = (int32_t)min(max(start + count, (int64_t)0), cap);
-    // the unit's rows that exist: from .. to - 1
+    if (unit == 0 && part == 0 && threadIdx.x == 0 && a.lens) a.lens[b] = (int32_t)min(max(start + count, (int64_t)0), cap);
+    // the unit's first row of the cache, and the token that becomes it
+    const int64_t row0 = (start >> 5) * kAppendRows + (int64_t)unit * kAppendRows;
+    const int64_t tok0 = row0 - start;
+    // its rows whose tokens exist: from .. to - 1; all of them are rows of the cache or none: a cache begins and ends with a unit
     const int from = (int)min(max(-tok0, (int64_t)0), (int64_t)kAppendRows);
-    int64_t end = count - tok0;
-    if (keys) end = min(end, cap - row0);
-    const int to = (int)min(max(end, (int64_t)0), (int64_t)kAppendRows);
+    const int to = (int)min(max(count - tok0, (int64_t)0), (int64_t)kAppendRows);
     if (from >= to) continue;
-    const int page = keys ? ((ScalarInts)a.pages)[(int64_t)b * a.max_pages + row0 / kTileRows] : 0;
-    if (keys && (page < 0 || page >= a.n_pages)) continue;
+    int page = -1;
+    if (row0 >= 0 && row0 < cap) page = ((ScalarInts)a.pages)[(int64_t)b * a.max_pages + row0 / kTileRows];
+    const int k_heads = a.H_kv, heads = a.H_kv + a.q_heads;
+    const bool stored = page >= 0 && page < a.n_pages;
 
-    // a head's rows are requested a head ahead, the first ones before the table of turns is worked out
-    const int which = keys ? 1 : 0;
-    const int H = keys ? a.H_kv : r.H;
+    // heads: those of the keys, then those of the queries
     const int64_t tok_first = (int64_t)b * T + tok0;
-    const uint16_t* const in = r.in[which] + (tok_first + row8) * r.stride[which] + c0;
-    const uint16_t* const in_v = a.V + (tok_first + row8) * a.v_stride + c0;
     u32x4 raw[4], val[4];
     auto exists = [&](int i) { return 8 * i + row8 >= from && 8 * i + row8 < to; };
     auto request = [&](int h, int i) {
-      raw[i] = u32x4{0u, 0u, 0u, 0u};
-      if (exists(i)) raw[i] = *reinterpret_cast<const u32x4*>(in + 8 * i * r.stride[which] + h * kHeadDim);
+      const int t = h < k_heads ? 1 : 0;
+      const int64_t stride = r.stride[t];
+      if (exists(i))
+        raw[i] = *reinterpret_cast<const u32x4*>(r.in[t] + (tok_first + 8 * i) * stride + (t ? h : h - k_heads) * kHeadDim +
+                                                 (row8 * stride + c0));
     };
     auto request_v = [&](int h, int i) {
-      val[i] = u32x4{0u, 0u, 0u, 0u};
-      if (exists(i)) val[i] = *reinterpret_cast<const u32x4*>(in_v + 8 * i * a.v_stride + h * kHeadDim);
+      if (h < k_heads && exists(i))
+        val[i] = *reinterpret_cast<const u32x4*>(a.V + (tok_first + 8 * i) * a.v_stride + h * kHeadDim + (row8 * a.v_stride + c0));
     };
-    const int step = (int)parts * kAppendWaves;
+    const int step = a.parts * kAppendWaves;
     int h = part * kAppendWaves + wave;
+    if (!stored)  // nothing of the keys is kept
+      while (h < k_heads) h += step;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      if (h < H) request(h, i);
-      if (keys && h < H) request_v(h, i);
+      raw[i] = val[i] = u32x4{0u, 0u, 0u, 0u};
+      if (h < heads) request(h, i);
+      if (h < heads) request_v(h, i);
     }
-    ch.kind = r.norm[which].kind;
-    ch.eps = r.norm[which].eps;
-    load8(r.norm[which].gamma, c0, 1.f, ch.gamma);
-    load8(r.norm[which].beta, c0, 0.f, ch.beta);
 
-    if (r.pairs) {
-      __syncthreads();  // the last unit's reads are done
+    __syncthreads();  // the last unit's reads are done
+    if constexpr (kPairs != kNoPairs) {
+      // this thread's pair of every eighth row's
+      const int p = threadIdx.x % (kHeadDim / 2);
       if (p < r.pairs) {
+        const int axis = r.axis[p], lo = r.first[p], hi = r.second[p];
+        const uint64_t freq = r.freq[p];
         for (int row = from + threadIdx.x / (kHeadDim / 2); row < to; row += kAppendThreads / (kHeadDim / 2)) {
           const uint32_t tok = (uint32_t)(tok0 + row);
           int32_t pos;
@@ -164,41 +200,43 @@ __global__ __launch_bounds__(kAppendThreads, 3) void append_kernel(AppendArgs a)
           const uint64_t phase = (uint64_t)(int64_t)pos * freq;
           float s, c;
           sincospif((float)(int32_t)(phase >> 32) * 0x1p-31f, &s, &c);
-          turns[row][lo] = f32x2{c, -s};
-          turns[row][hi] = f32x2{c, s};
+          table[table_at(row, lo)] = f32x2{c, -s};
+          table[table_at(row, hi)] = f32x2{c, s};
         }
       }
-      __syncthreads();
     }
+    __syncthreads();
 
-    for (; h < H; h += step) {
+    for (; h < heads; h += step) {
+      const bool key = h < k_heads;
+      const SeamNorm& norm = r.norm[key ? 1 : 0];
       const int64_t tile = ((int64_t)page * a.H_kv + h) * kTileElems + (row0 % kTileRows) * kHeadDim;
-      // values, row-major with the upper half of a row's chunks exchanged with the lower on rows 2 and 3 mod 4 (the
-      // transposing read's four rows then lie on different banks)
-      lds_char* const v = (lds_char*)values[wave];
-      if (keys) {
-        wave_lds_fence();
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int row = 8 * i + row8;
-          *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(v + row * 128 + (j ^ (4 * ((row >> 1) & 1))) * 16) = val[i];
-          if (h + step < H) request_v(h + step, i);
-        }
-      }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if (8 * i >= to || 8 * i + 8 <= from) continue;
         const int row = 8 * i + row8;
         float x[8];
         unpack8(raw[i], x);
-        if (h + step < H) request(h + step, i);
-        turn8(x, ch, r.pairs != 0, c0, head, turns[row]);
+        if (h + step < heads) request(h + step, i);
+        if (norm.kind != AGG_NORM_NONE) norm8(x, norm.kind, norm.eps, affine[key ? 1 : 0] + c0);
+        turn8<kPairs>(x, ch, lane, row, turns, (float*)space[wave]);
         if (exists(i)) {
-          uint16_t* const at = keys ? a.Kc + tile + (j * 32 + row) * 8 : r.out[0] + ((tok_first + row) * H + h) * kHeadDim + c0;
+          uint16_t* const at = key ? a.Kc + tile + (j * 32 + row) * 8
+                                   : r.out[0] + ((tok_first + row) * a.q_heads + (h - k_heads)) * kHeadDim + c0;
           *reinterpret_cast<u32x4*>(at) = pack8(x);
         }
       }
-      if (!keys) continue;
+      if (!key) continue;
+      // values, row-major with the upper half of a row's chunks exchanged with the lower on rows 2 and 3 mod 4 (the
+      // transposing read's four rows then lie on different banks)
+      lds_char* const v = (lds_char*)space[wave];
+      wave_lds_fence();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int row = 8 * i + row8;
+        *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(v + row * 128 + (j ^ (4 * ((row >> 1) & 1))) * 16) = val[i];
+        if (h + step < heads) request_v(h + step, i);
+      }
       wave_lds_fence();
       const int c = lane & 15, G = lane >> 4;
       const int k0 = 16 * (G >> 1) + 4 * (G & 1);  // first row of this lane's chunks: k0 .. + 3, k0 + 8 .. + 11
@@ -220,33 +258,47 @@ __global__ __launch_bounds__(kAppendThreads, 3) void append_kernel(AppendArgs a)
           }
         }
       }
+      wave_lds_fence();  // the reads are done before the next rows come
     }
   }
+}
+
+// Where the pairs of a rotation lie, seen from a lane of eight channels.
+static int pairs_kind(const RopeArgs& r) {
+  if (!r.pairs) return kNoPairs;
+  bool in_lane = true, across = true;
+  for (int c = 0; c < kHeadDim; ++c) {
+    if (!(r.other[c] & 0x80)) continue;
+    const int other = r.other[c] & 63;
+    in_lane = in_lane && other == (c ^ 1);
+    // all eight channels of a lane turn, with those of one lane in the same order
+    across = across && other % 8 == c % 8 && (r.other[c & ~7] & 0x80) && (r.other[c & ~7] & 63) / 8 == other / 8;
+  }
+  return in_lane ? kPairsInLane : across ? kPairsAcrossLanes : kPairsAnywhere;
 }
 
 hipError_t launch_append(const AppendArgs& args, hipStream_t st) {
   AppendArgs a = args;
   const int64_t T = a.r.NQ;
+  a.q_heads = a.r.in[0] ? a.r.H : 0;
   // a sequence's tokens lie in one more half page than they fill where they begin inside one
-  a.k_units = (int32_t)((T + kAppendRows - 1) / kAppendRows + 1);
-  a.q_units = a.r.in[0] ? (int32_t)((T + kAppendRows - 1) / kAppendRows) : 0;
+  a.units = (int32_t)((T + kAppendRows - 1) / kAppendRows + 1);
   // few rows: their heads are shared out while all workgroups still run at once
   constexpr int64_t kAtOnce = 256 * 3;
-  auto share = [&](int64_t units, int heads) {
-    int parts = 1;
-    const int most = (heads + kAppendWaves - 1) / kAppendWaves;
-    while (parts < most && units * (parts + 1) <= kAtOnce) ++parts;
-    return parts;
-  };
-  a.k_parts = share((int64_t)a.B * (a.k_units + a.q_units), a.H_kv);
-  a.q_parts = share((int64_t)a.B * (a.k_units + a.q_units), a.r.H);
-  a.k_items = (int64_t)a.B * a.k_units * a.k_parts;
-  a.q_items = (int64_t)a.B * a.q_units * a.q_parts;
-  if (a.k_items > 0xFFFFFFFFll || a.q_items > 0xFFFFFFFFll) return hipErrorInvalidConfiguration;
-  const int64_t items = a.k_items + a.q_items;
+  const int most = (int)(((int64_t)a.H_kv + a.q_heads + kAppendWaves - 1) / kAppendWaves);
+  a.parts = 1;
+  while (a.parts < most && (int64_t)a.B * a.units * (a.parts + 1) <= kAtOnce) ++a.parts;
+  a.items = (int64_t)a.B * a.units * a.parts;
+  if (a.items > 0xFFFFFFFFll) return hipErrorInvalidConfiguration;
   constexpr int64_t kMost = 1 << 20;
+  const dim3 grid((unsigned)(a.items < kMost ? a.items : kMost)), block(kAppendThreads);
   (void)hipGetLastError();
-  hipLaunchKernelGGL(append_kernel, dim3((unsigned)(items < kMost ? items : kMost)), dim3(kAppendThreads), 0, st, a);
+  switch (pairs_kind(a.r)) {
+    case kNoPairs: hipLaunchKernelGGL(append_kernel<kNoPairs>, grid, block, 0, st, a); break;
+    case kPairsInLane: hipLaunchKernelGGL(append_kernel<kPairsInLane>, grid, block, 0, st, a); break;
+    case kPairsAcrossLanes: hipLaunchKernelGGL(append_kernel<kPairsAcrossLanes>, grid, block, 0, st, a); break;
+    default: hipLaunchKernelGGL(append_kernel<kPairsAnywhere>, grid, block, 0, st, a);
+  }
   return hipGetLastError();
 }
 

@@ -254,9 +254,9 @@ struct AppendArgs {
   const int32_t *start, *counts;
   int32_t* lens;
   int32_t B, H_kv, max_pages, n_pages;
-  // set by launch_append: pieces of 32 rows of a sequence and workgroups that share the heads of one, for keys and for queries
-  int64_t k_items, q_items;
-  int32_t k_units, q_units, k_parts, q_parts;
+  // set by launch_append: heads of queries, pieces of 32 rows of a sequence, workgroups that share the heads of one, of all
+  int32_t q_heads, units, parts;
+  int64_t items;
 };
 hipError_t launch_append(const AppendArgs& args, hipStream_t st);
 
