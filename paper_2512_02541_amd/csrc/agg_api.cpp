@@ -703,6 +703,7 @@ int make_append_args(const agg_cache* c, const agg_shape* shape, const agg_rope*
   Geom g;
   if ((rc = make_geom(&s, &g, true)) != AGG_OK) return rc;
   if (s.B != c->B || s.H % c->H != 0) return AGG_ERR_SHAPE;
+  if (s.H > (1 << 22)) return AGG_ERR_OVERFLOW;  // a few rows' heads are addressed with 32 bits
   memset(a, 0, sizeof *a);
   RopeArgs* r = &a->r;
   if ((rc = make_rope(rope, r)) != AGG_OK) return rc;

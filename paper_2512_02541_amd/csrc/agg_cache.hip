@@ -19,7 +19,6 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 // ---------------------------------------------------------------------------
 constexpr int kAppendThreads = 256;
 constexpr int kAppendWaves = kAppendThreads / 64;
-constexpr int kAppendRows = 32;
 
 namespace {
 
@@ -104,14 +103,15 @@ __device__ __forceinline__ void turn8(float (&x)[8], const Channels& ch, int lan
 
 }  // namespace
 
-template <int kPairs>
-__global__ __launch_bounds__(kAppendThreads, 3) void append_kernel(AppendArgs a) {
-  __shared__ __align__(16) f32x4 turns[kAppendRows * 32];
+template <int kPairs, int kRows>
+__global__ __launch_bounds__(kAppendThreads, kPairs == kPairsAnywhere && kRows == 32 ? 3 : 4) void append_kernel(AppendArgs a) {
+  __shared__ __align__(16) f32x4 turns[kRows * 32];
   // of a wavefront: eight rows of a head while they are turned, then a head's values while they are transposed
-  __shared__ __align__(16) uint16_t space[kAppendWaves][kAppendRows * kHeadDim];
+  __shared__ __align__(16) uint16_t space[kAppendWaves][kRows == 32 ? kRows * kHeadDim : 1024];
   __shared__ __align__(16) float affine[2][2 * kHeadDim];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 15, G = lane >> 4;
   const int row8 = lane >> 3, j = lane & 7, c0 = j * 8;  // this lane's row of eight, chunk of a head, first channel
   const RopeArgs& r = a.r;
   const int T = (int)r.NQ;
@@ -121,6 +121,10 @@ __global__ __launch_bounds__(kAppendThreads, 3) void append_kernel(AppendArgs a)
   ch.other[0] = (uint32_t)others;
   ch.other[1] = (uint32_t)(others >> 32);
   ch.lane_at = ((lane & 56) + (int)((others >> 3) & 7)) * 4;
+  // this thread's pair of every eighth row's (requested here: the arguments lie far away)
+  const int p = threadIdx.x % (kHeadDim / 2);
+  const int axis = r.axis[p], lo = r.first[p], hi = r.second[p];
+  const uint64_t freq = r.freq[p];
   if (threadIdx.x < 2 * kHeadDim) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -141,11 +145,11 @@ __global__ __launch_bounds__(kAppendThreads, 3) void append_kernel(AppendArgs a)
     const int64_t cap = (int64_t)a.max_pages * kTileRows;
     if (unit == 0 && part == 0 && threadIdx.x == 0 && a.lens) a.lens[b] = (int32_t)min(max(start + count, (int64_t)0), cap);
     // the unit's first row of the cache, and the token that becomes it
-    const int64_t row0 = (start >> 5) * kAppendRows + (int64_t)unit * kAppendRows;
+    const int64_t row0 = (start >> (kRows == 32 ? 5 : 4)) * kRows + (int64_t)unit * kRows;
     const int64_t tok0 = row0 - start;
     // its rows whose tokens exist: from .. to - 1; all of them are rows of the cache or none: a cache begins and ends with a unit
-    const int from = (int)min(max(-tok0, (int64_t)0), (int64_t)kAppendRows);
-    const int to = (int)min(max(count - tok0, (int64_t)0), (int64_t)kAppendRows);
+    const int from = (int)min(max(-tok0, (int64_t)0), (int64_t)kRows);
+    const int to = (int)min(max(count - tok0, (int64_t)0), (int64_t)kRows);
     if (from >= to) continue;
     int page = -1;
     if (row0 >= 0 && row0 < cap) page = ((ScalarInts)a.pages)[(int64_t)b * a.max_pages + row0 / kTileRows];
@@ -154,7 +158,7 @@ __global__ __launch_bounds__(kAppendThreads, 3) void append_kernel(AppendArgs a)
 
     // heads: those of the keys, then those of the queries
     const int64_t tok_first = (int64_t)b * T + tok0;
-    u32x4 raw[4], val[4];
+    u32x4 raw[kRows / 8], val[kRows / 8];
     auto exists = [&](int i) { return 8 * i + row8 >= from && 8 * i + row8 < to; };
     auto request = [&](int h, int i) {
       const int t = h < k_heads ? 1 : 0;
@@ -167,24 +171,24 @@ __global__ __launch_bounds__(kAppendThreads, 3) void append_kernel(AppendArgs a)
       if (h < k_heads && exists(i))
         val[i] = *reinterpret_cast<const u32x4*>(a.V + (tok_first + 8 * i) * a.v_stride + h * kHeadDim + (row8 * a.v_stride + c0));
     };
+    // this lane's place behind a uniform one, of keys, of queries and of values
+    const uint32_t k_lane = (uint32_t)(j * 32 + row8) * 8, q_lane = (uint32_t)row8 * (uint32_t)a.q_heads * kHeadDim + c0,
+                   v_lane = (uint32_t)(kRows == 32 ? G * 64 + c : (G & 1) * 64 + (G >> 1) * 32 + c) * 8;
+    const int in_page = (int)(row0 & (kTileRows - 1));
     const int step = a.parts * kAppendWaves;
     int h = part * kAppendWaves + wave;
     if (!stored)  // nothing of the keys is kept
       while (h < k_heads) h += step;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kRows / 8; ++i) {
       raw[i] = val[i] = u32x4{0u, 0u, 0u, 0u};
       if (h < heads) request(h, i);
       if (h < heads) request_v(h, i);
     }
 
-    __syncthreads();  // the last unit's reads are done
+    lds_barrier();  // the last unit's reads are done; rows stay on their way
     if constexpr (kPairs != kNoPairs) {
-      // this thread's pair of every eighth row's
-      const int p = threadIdx.x % (kHeadDim / 2);
       if (p < r.pairs) {
-        const int axis = r.axis[p], lo = r.first[p], hi = r.second[p];
-        const uint64_t freq = r.freq[p];
         for (int row = from + threadIdx.x / (kHeadDim / 2); row < to; row += kAppendThreads / (kHeadDim / 2)) {
           const uint32_t tok = (uint32_t)(tok0 + row);
           int32_t pos;
@@ -198,21 +202,21 @@ __global__ __launch_bounds__(kAppendThreads, 3) void append_kernel(AppendArgs a)
             else pos = r.patch0 + (axis == 1 ? patch / r.n_w : patch % r.n_w);
           }
           const uint64_t phase = (uint64_t)(int64_t)pos * freq;
-          float s, c;
-          sincospif((float)(int32_t)(phase >> 32) * 0x1p-31f, &s, &c);
-          table[table_at(row, lo)] = f32x2{c, -s};
-          table[table_at(row, hi)] = f32x2{c, s};
+          float sine, cosine;
+          sincospif((float)(int32_t)(phase >> 32) * 0x1p-31f, &sine, &cosine);
+          table[table_at(row, lo)] = f32x2{cosine, -sine};
+          table[table_at(row, hi)] = f32x2{cosine, sine};
         }
       }
     }
-    __syncthreads();
+    lds_barrier();
 
     for (; h < heads; h += step) {
       const bool key = h < k_heads;
       const SeamNorm& norm = r.norm[key ? 1 : 0];
-      const int64_t tile = ((int64_t)page * a.H_kv + h) * kTileElems + (row0 % kTileRows) * kHeadDim;
+      const int64_t tile = ((int64_t)page * a.H_kv + h) * kTileElems;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < kRows / 8; ++i) {
         if (8 * i >= to || 8 * i + 8 <= from) continue;
         const int row = 8 * i + row8;
         float x[8];
@@ -221,9 +225,8 @@ __global__ __launch_bounds__(kAppendThreads, 3) void append_kernel(AppendArgs a)
         if (norm.kind != AGG_NORM_NONE) norm8(x, norm.kind, norm.eps, affine[key ? 1 : 0] + c0);
         turn8<kPairs>(x, ch, lane, row, turns, (float*)space[wave]);
         if (exists(i)) {
-          uint16_t* const at = key ? a.Kc + tile + (j * 32 + row) * 8
-                                   : r.out[0] + ((tok_first + row) * a.q_heads + (h - k_heads)) * kHeadDim + c0;
-          *reinterpret_cast<u32x4*>(at) = pack8(x);
+          uint16_t* const at = key ? a.Kc + tile + (in_page / 32 * 256 + in_page % 32 + 8 * i) * 8 : r.out[0] + ((tok_first + 8 * i) * a.q_heads + (h - k_heads)) * kHeadDim;
+          *reinterpret_cast<u32x4*>(at + (key ? k_lane : q_lane)) = pack8(x);
         }
       }
       if (!key) continue;
@@ -232,21 +235,22 @@ __global__ __launch_bounds__(kAppendThreads, 3) void append_kernel(AppendArgs a)
       lds_char* const v = (lds_char*)space[wave];
       wave_lds_fence();
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < kRows / 8; ++i) {
         const int row = 8 * i + row8;
         *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(v + row * 128 + (j ^ (4 * ((row >> 1) & 1))) * 16) = val[i];
         if (h + step < heads) request_v(h + step, i);
       }
       wave_lds_fence();
-      const int c = lane & 15, G = lane >> 4;
-      const int k0 = 16 * (G >> 1) + 4 * (G & 1);  // first row of this lane's chunks: k0 .. + 3, k0 + 8 .. + 11
-      const int row = k0 + (c >> 2);               // its row of the four that the read transposes
+      // 32 rows: the lanes' groups of sixteen take the chunks of 16 rows and of four in them; 16 rows: halves of the channels
+      const int k0 = (kRows == 32 ? 16 * (G >> 1) : 0) + 4 * (G & 1);  // first row of this lane's chunks: k0 .. + 3, k0 + 8 .. + 11
+      const int row = k0 + (c >> 2);                                  // its row of the four that the read transposes
 #pragma unroll
-      for (int dt = 0; dt < 4; ++dt) {
+      for (int d = 0; d < kRows / 8; ++d) {
+        const int dt = kRows == 32 ? d : 2 * (G >> 1) + d;
         lds_char* const at = v + row * 128 + ((2 * dt + ((c & 3) >> 1)) ^ (4 * ((row >> 1) & 1))) * 16 + (c & 1) * 8;
         const s16x4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
         const s16x4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + 8 * 128));
-        uint16_t* const to_page = a.Vc + tile + (G * 64 + 16 * dt + c) * 8;
+        uint16_t* const to_page = a.Vc + tile + in_page * kHeadDim + d * 128 + v_lane;
         if (k0 >= from && k0 + 11 < to) {
           const u32x2 l2 = __builtin_bit_cast(u32x2, x0), h2 = __builtin_bit_cast(u32x2, x1);
           *reinterpret_cast<u32x4*>(to_page) = u32x4{l2[0], l2[1], h2[0], h2[1]};
@@ -277,28 +281,36 @@ static int pairs_kind(const RopeArgs& r) {
   return in_lane ? kPairsInLane : across ? kPairsAcrossLanes : kPairsAnywhere;
 }
 
+template <int kRows>
+static void launch_rows(const AppendArgs& a, hipStream_t st) {
+  constexpr int64_t kMost = 1 << 20;
+  const dim3 grid((unsigned)(a.items < kMost ? a.items : kMost)), block(kAppendThreads);
+  switch (pairs_kind(a.r)) {
+    case kNoPairs: hipLaunchKernelGGL((append_kernel<kNoPairs, kRows>), grid, block, 0, st, a); break;
+    case kPairsInLane: hipLaunchKernelGGL((append_kernel<kPairsInLane, kRows>), grid, block, 0, st, a); break;
+    case kPairsAcrossLanes: hipLaunchKernelGGL((append_kernel<kPairsAcrossLanes, kRows>), grid, block, 0, st, a); break;
+    default: hipLaunchKernelGGL((append_kernel<kPairsAnywhere, kRows>), grid, block, 0, st, a);
+  }
+}
+
 hipError_t launch_append(const AppendArgs& args, hipStream_t st) {
   AppendArgs a = args;
   const int64_t T = a.r.NQ;
   a.q_heads = a.r.in[0] ? a.r.H : 0;
-  // a sequence's tokens lie in one more half page than they fill where they begin inside one
-  a.units = (int32_t)((T + kAppendRows - 1) / kAppendRows + 1);
-  // few rows: their heads are shared out while all workgroups still run at once
-  constexpr int64_t kAtOnce = 256 * 3;
   const int most = (int)(((int64_t)a.H_kv + a.q_heads + kAppendWaves - 1) / kAppendWaves);
+  // a sequence's tokens lie in one more piece than they fill where they begin inside one
+  auto units = [&](int rows) { return (T + rows - 1) / rows + 1; };
+  // few rows: pieces of 16 and heads of their own for every wavefront, while all workgroups still run at once
+  constexpr int64_t kAtOnce = 256 * 4;
+  const bool few = a.B * units(16) * most <= kAtOnce;
+  a.units = (int32_t)units(few ? 16 : 32);
   a.parts = 1;
   while (a.parts < most && (int64_t)a.B * a.units * (a.parts + 1) <= kAtOnce) ++a.parts;
   a.items = (int64_t)a.B * a.units * a.parts;
   if (a.items > 0xFFFFFFFFll) return hipErrorInvalidConfiguration;
-  constexpr int64_t kMost = 1 << 20;
-  const dim3 grid((unsigned)(a.items < kMost ? a.items : kMost)), block(kAppendThreads);
   (void)hipGetLastError();
-  switch (pairs_kind(a.r)) {
-    case kNoPairs: hipLaunchKernelGGL(append_kernel<kNoPairs>, grid, block, 0, st, a); break;
-    case kPairsInLane: hipLaunchKernelGGL(append_kernel<kPairsInLane>, grid, block, 0, st, a); break;
-    case kPairsAcrossLanes: hipLaunchKernelGGL(append_kernel<kPairsAcrossLanes>, grid, block, 0, st, a); break;
-    default: hipLaunchKernelGGL(append_kernel<kPairsAnywhere>, grid, block, 0, st, a);
-  }
+  if (few) launch_rows<16>(a, st);
+  else launch_rows<32>(a, st);
   return hipGetLastError();
 }
 

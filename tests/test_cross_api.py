@@ -174,6 +174,7 @@ def test_append_refusals():
                 dict(kn=agg.make_norm(agg.AGG_NORM_LAYER, 1e-5, FAKE + 4))):
         assert _append(**bad) == A, bad
     assert _append(t0=2 ** 31 - 1) == O and _append(patch0=2 ** 31 - 3) == O and _append(ks=1 << 56) == O
+    assert _append(HQ=(1 << 22) + 2) == O
     lib = agg.lib()
     c = agg.agg_cache(9, 2, 64, 2, 2, at(10), at(11), at(12))
     assert lib.agg_cache_append(agg.ctypes.byref(c), None, None, None, None, None, None, 0, at(1), 0, at(2), 0, None, None, None, None,
@@ -272,15 +273,26 @@ def test_kernels_leave_m0_to_their_copy_statements(assembly):
     assert not offenders, offenders[:5]
 
 
+def metadata(text, kernels):
+    """(name, fields) of the kernels whose mangled names hold `kernels`."""
+    for kernel in re.split(r"^  - \.", text, flags=re.M):
+        name = re.search(r"\.name: +\S*(%s\S*)" % kernels, kernel)
+        if name:
+            yield name.group(1), {f: int(re.search(r"\.%s: +(\d+)" % f, kernel).group(1))
+                                  for f in ("vgpr_spill_count", "private_segment_fixed_size")}
+
+
 def test_kernels_do_not_spill(assembly):
     """The wide kernels hold two paths' code: nothing of the second may lie in scratch memory while the first runs."""
-    seen, spilled = 0, []
-    for kernel in re.split(r"^  - \.", assembly, flags=re.M):
-        name = re.search(r"\.name: +\S*(cross_\w+_kernel\S*)", kernel)
-        if name:
-            seen += 1
-            field = {f: int(re.search(r"\.%s: +(\d+)" % f, kernel).group(1))
-                     for f in ("vgpr_spill_count", "private_segment_fixed_size")}
-            if any(field.values()):
-                spilled.append((name.group(1), field))
-    assert seen >= 12 and not spilled, spilled
+    found = list(metadata(assembly, r"cross_\w+_kernel"))
+    assert len(found) >= 12 and not [x for x in found if any(x[1].values())]
+
+
+def test_append_kernels_do_not_spill(tmp_path):
+    out = tmp_path / "agg_cache.s"
+    subprocess.check_call([b.HIPCC, *b.FLAGS, "-I", os.path.join(b.ROOT, "include"), "-I", b.CSRC, "-S", "--cuda-device-only",
+                           os.path.join(b.CSRC, "agg_cache.hip"), "-o", str(out)], stderr=subprocess.DEVNULL)
+    text = out.read_text()
+    found = list(metadata(text, "append_kernel"))
+    assert len(found) == 8 and not [x for x in found if x[1]["vgpr_spill_count"]]
+    assert "scratch_load" not in text and "scratch_store" not in text  # (scalar registers may spill, to lanes of a vector register)

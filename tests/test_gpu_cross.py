@@ -378,10 +378,17 @@ def append_case(shape, H_kv, start=None, counts=None, pairing=agg.AGG_ROPE_SECTI
     for b in range(B):
         want, tol = turned(f64(k[b]), k_spec, at[b], pairing, ax, float(np.float32(base)))
         want, tol = (torch.tensor(x, device="cuda") for x in (want, tol))
-        for t in range(number[b]):
-            orc.store(exp_v, pages, orc.v_place, b, s0[b] + t, v[b, t])
-            orc.store(exp_k, pages, orc.k_place, b, s0[b] + t, want[t])
-            orc.store(tol_k, pages, orc.k_place, b, s0[b] + t, tol[t])
+        tokens = torch.arange(number[b], device="cuda")
+        rows = s0[b] + tokens
+        inside = (rows >= 0) & (rows < 64 * cap)
+        rows, tokens = rows[inside], tokens[inside]
+        page = pages[b, rows // 64].long()
+        inside = (page >= 0) & (page < n)
+        rows, tokens, page = rows[inside], tokens[inside], page[inside][:, None]
+        for h in range(H_kv):
+            exp_v[page, h, orc._places(orc.v_place, "cuda")[rows % 64]] = v[b, tokens, h]
+            exp_k[page, h, orc._places(orc.k_place, "cuda")[rows % 64]] = want[tokens, h]
+            tol_k[page, h, orc._places(orc.k_place, "cuda")[rows % 64]] = tol[tokens, h]
         if queries:
             want, tol = turned(f64(q[b]), q_spec, at[b], pairing, ax, float(np.float32(base)))
             c = number[b]
@@ -426,6 +433,14 @@ def test_append_given_positions_and_parts_left_out():
     append_case(frames(2, 1, 5, 5, 1, 4), 4, [1, 2], given=True, pairing=agg.AGG_ROPE_HEAD, axes=(16, 24, 24))
     append_case(frames(2, 1, 5, 5, 1, 4), 4, None, rope=False, kind="rms")
     append_case(frames(2, 1, 5, 5, 1, 4), 2, [62, 3], rope=False, kind="none", strided=True)
+
+
+@pytest.mark.parametrize("pairing, axes", [(agg.AGG_ROPE_SECTIONS, (0, 32, 32)), (agg.AGG_ROPE_NEIGHBOURS, (16, 24, 24)),
+                                           (agg.AGG_ROPE_SECTIONS, (20, 22, 14)), (agg.AGG_ROPE_HEAD, (0, 0, 0))])
+def test_append_many_rows(pairing, axes):
+    """More rows than pieces of 16 take: pieces of 32, beginning and ending inside one."""
+    append_case(frames(3, 2, 37, 37, 5, 3), 3, [5, 49, 64], [2748, 1401, 2000], pairing=pairing, axes=axes, strided=True)
+    append_case(frames(3, 3, 37, 37, 5, 6), 2, [1, 31, 4000], None, pairing=pairing, axes=axes, kind="rms", max_pages=100, queries=axes[1] != 24)
 
 
 def test_append_a_frame():
