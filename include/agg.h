@@ -457,7 +457,7 @@ typedef struct agg_cross {
   const int32_t* k_lens; /* device int32 [B], clamped to 0 .. NK; NULL: NK                           */
 } agg_cross;
 
-/* Host only.  Scratch bytes that the two attention calls below need for these sizes (0: none, the pointer may be NULL; 0 too on
+/* Host only.  Scratch bytes that the two attention calls below need for this struct (0: none, the pointer may be NULL; 0 too on
  * invalid sizes).  Calls that may overlap in time need a workspace each, as do graphs that are replayed side by side. */
 size_t agg_cross_workspace_bytes(const agg_cross* cross);
 

@@ -650,7 +650,7 @@ int make_cross_args(const agg_cross* c, const agg_cache* cache, const void* Q, i
   if (misaligned(Q) || misaligned(K) || misaligned(V) || misaligned(O) || misaligned(workspace) || misaligned4(lse) ||
       misaligned4(c->q_lens) || misaligned4(c->k_lens))
     return AGG_ERR_ALIGN;
-  const size_t need = cross_partial_floats(c->B, c->NQ, c->NK, c->H, c->H_kv) * sizeof(float);
+  const size_t need = cross_partial_floats(c->B, c->NQ, c->NK, c->H, c->H_kv, cross_ragged(c->B, c->q_lens, c->k_lens)) * sizeof(float);
   if (need > 0 && !workspace) return AGG_ERR_NULL;
   if (workspace_bytes < need) return AGG_ERR_WORKSPACE;
   // what the call writes may overlap nothing else of it
@@ -825,7 +825,8 @@ int agg_mx4_linear_fwd(int64_t rows, int32_t N, int32_t K, const agg_mx4_linear*
 
 size_t agg_cross_workspace_bytes(const agg_cross* cross) {
   if (check_cross(cross) != AGG_OK) return 0;
-  return cross_partial_floats(cross->B, cross->NQ, cross->NK, cross->H, cross->H_kv) * sizeof(float);
+  const bool ragged = cross_ragged(cross->B, cross->q_lens, cross->k_lens);
+  return cross_partial_floats(cross->B, cross->NQ, cross->NK, cross->H, cross->H_kv, ragged) * sizeof(float);
 }
 
 int agg_cross_attn_fwd(const agg_cross* cross, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,

@@ -82,8 +82,6 @@ struct AttnArgs {
   int64_t list_stride;   // 0 when every batch element uses the same list
 };
 
-constexpr int kTileLds = 2 * kLdsTiles * kTileElems;  // elements: K tiles, then V tiles
-
 // One workgroup's queries q_begin .. q_end - 1 (at most what four wavefronts hold) by one of the
 // two paths.  Returns false, without storing anything, when the fast path met a row it cannot
 // handle.
@@ -95,7 +93,6 @@ constexpr int kTileLds = 2 * kLdsTiles * kTileElems;  // elements: K tiles, then
 //               accumulators just add: the second group's go through LDS to the first, which
 //               finishes the rows.
 //   kTwin       eight: both groups do the same (so that their barriers match), the first stores.
-enum { kAlone, kSplitKeys, kTwin };
 template <int kSrc, bool kGen, int kQB, int kJ, int kMode = kAlone>
 __device__ __forceinline__ bool attend(const AttnArgs& p, uint16_t* tiles, uint32_t* votes, int b, int h,
                                        int64_t q_begin, int64_t q_end) {

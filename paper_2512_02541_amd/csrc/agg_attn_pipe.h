@@ -676,6 +676,12 @@ __device__ __forceinline__ bool key_loop(Wave<kQB, kJ>& w, u32x4* __restrict__ l
   return true;
 }
 
+constexpr int kTileLds = 2 * kLdsTiles * kTileElems;  // elements: K tiles, then V tiles
+
+// Wavefronts of a workgroup: four; eight, of which four take the first half of the keys and four the second; eight that all do the
+// same, so that their barriers match, the first four of which store.
+enum { kAlone, kSplitKeys, kTwin };
+
 // position in a launch list of n tiles per pair -> (pair, tile of the pair).  Consecutive ids go
 // to consecutive XCDs.  Whole pairs are dealt out one per XCD, so that an XCD streams one
 // key/value set at a time through its own L2; the npairs % 8 pairs that are left share the XCDs

@@ -259,15 +259,20 @@ __global__ __launch_bounds__(kFewThreads, kJ == 1 ? 4 : 2) void cross_few_kernel
 namespace {
 
 // One workgroup's rows row_begin .. row_end - 1 of pair (b, hk) over its split's keys, by one of the two paths.  Returns false, without
-// storing anything, when the fast path met a row it cannot handle.
-template <int kSrc, bool kGen, int kQB, int kJ>
+// storing anything, when the fast path met a row it cannot handle.  tiles: kTileLds elements of LDS per four wavefronts.
+template <int kSrc, bool kGen, int kQB, int kJ, int kMode = kAlone>
 __device__ __forceinline__ bool attend_cross(const CrossArgs& p, const CrossPlan& plan, int64_t pairs, uint16_t* tiles, uint32_t* votes,
                                              int64_t pair, int split, uint32_t row_begin, uint32_t row_end) {
   constexpr int kWaveQ = wave_queries(kQB, kJ);
   // (opaque on the general path, so that it holds nothing of the fast path's: agg_attn.hip)
-  int tid = threadIdx.x;
-  if (kGen) asm volatile("" : "+v"(tid));
-  u32x4* lds = reinterpret_cast<u32x4*>(tiles);
+  int thread = threadIdx.x;
+  if (kGen) asm volatile("" : "+v"(thread));
+  constexpr bool kSplit = kMode == kSplitKeys;
+  static_assert(!(kGen && kSplit), "the general path's halves would need a common reference");
+  const int group = kMode != kAlone ? __builtin_amdgcn_readfirstlane(thread / kAttnThreads) : 0;
+  const int tid = thread - group * kAttnThreads;
+  uint16_t* const smem = tiles + group * kTileLds;
+  u32x4* lds = reinterpret_cast<u32x4*>(smem);
   const int lane = tid & 63, wave = tid >> 6, c = lane & 15, G = lane >> 4;
   const FragAddr fa = frag_addr(lane);
   const int b = (int)(pair / p.H_kv), hk = (int)(pair % p.H_kv);
@@ -275,8 +280,13 @@ __device__ __forceinline__ bool attend_cross(const CrossArgs& p, const CrossPlan
   // this workgroup's key tiles
   const int n = cross_keys(p, b);
   const int64_t all = ((int64_t)n + kTileRows - 1) / kTileRows;
-  const int skip = (int)(all * split / plan.splits);
-  const int ntiles = (int)(all * (split + 1) / plan.splits) - skip;
+  int skip = (int)(all * split / plan.splits);
+  int ntiles = (int)(all * (split + 1) / plan.splits) - skip;
+  const int half = kSplit ? (ntiles + 1) / 2 : ntiles;
+  if (kSplit) {
+    ntiles = group ? ntiles - half : half;
+    skip += group ? half : 0;
+  }
   const int rows_here = min(n - skip * kTileRows, ntiles * kTileRows);
   const int last_valid = rows_here - (ntiles - 1) * kTileRows;  // 1..64
   KvSource src;
@@ -357,7 +367,35 @@ __device__ __forceinline__ bool attend_cross(const CrossArgs& p, const CrossPlan
       }
     }
   };
-  const bool done = key_loop<kSrc, kGen, false, kQB, kJ>(w, lds, votes, src, ntiles, last_valid, tid, wave, fa, G, first_tile);
+  bool done = true;
+  if (!kSplit || ntiles > 0)
+    done = key_loop<kSrc, kGen, kSplit, kQB, kJ>(w, lds, votes, src, ntiles, last_valid, tid, wave, fa, G, first_tile);
+  if (kSplit) {
+    // a loop passes one barrier per tile: the shorter one makes up for its missing tile.  Without a reference the two halves'
+    // sums and accumulators just add: the second group's go through its LDS, [register][wavefront][lane], to the first
+    if (ntiles < half) lds_barrier();
+    __syncthreads();  // both groups are done with their tiles
+    f32x4* over = reinterpret_cast<f32x4*>(tiles + kTileLds) + tid;
+    float* over_l = reinterpret_cast<float*>(tiles + kTileLds) + kQB * kJ * 4 * 4 * kAttnThreads + tid;
+    static_assert(!kSplit || kQB * kJ * (4 * 16 + 4) * kAttnThreads <= kTileLds * 2, "fits the group's LDS");
+    if (group) {
+#pragma unroll
+      for (int i = 0; i < kQB * kJ; ++i) {
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt) over[(4 * i + dt) * kAttnThreads] = w.O[i / kJ][i % kJ][dt];
+        over_l[i * kAttnThreads] = w.L[i / kJ][i % kJ][0];
+      }
+    }
+    __syncthreads();
+    if (!group) {
+#pragma unroll
+      for (int i = 0; i < kQB * kJ; ++i) {
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt) w.O[i / kJ][i % kJ][dt] += over[(4 * i + dt) * kAttnThreads];
+        w.L[i / kJ][i % kJ][0] += over_l[i * kAttnThreads];
+      }
+    }
+  }
 
   float l_fin[kQB][kJ];
   bool unsafe = false;
@@ -366,14 +404,15 @@ __device__ __forceinline__ bool attend_cross(const CrossArgs& p, const CrossPlan
 #pragma unroll
     for (int j = 0; j < kJ; ++j) {
       l_fin[qb][j] = kGen ? quad_sum(w.la[qb][j]) : __shfl(w.L[qb][j][0], c);
-      unsafe = unsafe || !(l_fin[qb][j] < kSumHi) || !(l_fin[qb][j] > kSumLo);
+      unsafe = unsafe || (group == 0 && (!(l_fin[qb][j] < kSumHi) || !(l_fin[qb][j] > kSumLo)));
     }
   if (!kGen) {
     if (!done) return false;
-    if (vote(unsafe, votes + kWaves, wave, lane, true)) return false;
+    if (vote(unsafe, votes + kWaves, wave, lane, group == 0)) return false;
   } else {
     __syncthreads();  // every wavefront is done with the tiles
   }
+  if (group) return true;
 
   int here = tid;
   asm volatile("" : "+v"(here));
@@ -395,7 +434,7 @@ __device__ __forceinline__ bool attend_cross(const CrossArgs& p, const CrossPlan
     return true;
   }
   // whole 128-byte rows, turned through a part of the tiles' LDS of the wavefront's own (agg_attn.hip)
-  uint16_t* epi = tiles + wave * (16 * kJ * kEpiStride);
+  uint16_t* epi = smem + wave * (16 * kJ * kEpiStride);
 #pragma unroll
   for (int qb = 0; qb < kQB; ++qb) {
     const uint32_t r0 = r_wave + qb * kJ * 16;
@@ -434,7 +473,7 @@ __device__ __forceinline__ void store_nothing(const CrossArgs& p, const CrossPla
                                               uint32_t row_begin, uint32_t row_end, bool no_keys) {
   const int b = (int)(pair / p.H_kv), hk = (int)(pair % p.H_kv), quad = threadIdx.x & 15;
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-  for (uint32_t row = row_begin + (threadIdx.x >> 4); row < row_end; row += kAttnThreads / 16) {
+  for (uint32_t row = row_begin + (threadIdx.x >> 4); row < row_end; row += blockDim.x / 16) {
     if (plan.splits == 1) {
       store_row(p, b, hk, row, quad, 0.f, 0.f, zero, no_keys);
       continue;
@@ -460,39 +499,66 @@ __device__ __forceinline__ const WideArgs& wide_args_again() {
   return *(const WideArgs*)args;
 }
 
-template <int kSrc, int kTail>
-__global__ __launch_bounds__(kAttnThreads, kBlocksPerCu) void cross_wide_kernel(WideArgs w) {
-  __shared__ __align__(16) uint16_t tiles[2 * kLdsTiles * kTileElems];
-  __shared__ __align__(16) uint32_t votes[kVoteWords];
+// What a workgroup does; false: nothing, or it is done.
+struct WideWork {
+  int pair, split;
+  uint32_t row_begin, row_end;
+};
+__device__ __forceinline__ bool wide_work(const WideArgs& w, int npairs, WideWork& x) {
   const CrossArgs& a = w.a;
-  const int npairs = a.B * a.H_kv;
   // the workgroups of a pair's split read the same keys: on one XCD they share them through its L2
   int unit, i;
-  if (!list_tile(tile_list(npairs * w.plan.splits, (int)w.plan.row_tiles), npairs * w.plan.splits, blockIdx.x, unit, i)) return;
-  const int pair = unit % npairs, split = unit / npairs, b = pair / a.H_kv;
+  if (!list_tile(tile_list(npairs * w.plan.splits, (int)w.plan.row_tiles), npairs * w.plan.splits, blockIdx.x, unit, i)) return false;
+  x.pair = unit % npairs;
+  x.split = unit / npairs;
+  const int b = x.pair / a.H_kv;
   const uint32_t rows = (uint32_t)cross_queries(a, b) * (uint32_t)a.group;
-  const uint32_t row_begin = (uint32_t)i * (uint32_t)w.plan.width;
-  if (row_begin >= rows) return;
-  const uint32_t row_end = min(rows, row_begin + (uint32_t)w.plan.width);
+  x.row_begin = (uint32_t)i * (uint32_t)w.plan.width;
+  if (x.row_begin >= rows) return false;
+  x.row_end = min(rows, x.row_begin + (uint32_t)w.plan.width);
   const int n = cross_keys(a, b);
   const int64_t all = ((int64_t)n + kTileRows - 1) / kTileRows;
-  if (all * split / w.plan.splits == all * (split + 1) / w.plan.splits) {
-    store_nothing(a, w.plan, npairs, pair, split, row_begin, row_end, n == 0);
-    return;
+  if (all * x.split / w.plan.splits == all * (x.split + 1) / w.plan.splits) {
+    store_nothing(a, w.plan, npairs, x.pair, x.split, x.row_begin, x.row_end, n == 0);
+    return false;
   }
+  return true;
+}
+
+template <int kSrc, int kTail>
+__global__ __launch_bounds__(kAttnThreads, kBlocksPerCu) void cross_wide_kernel(WideArgs w) {
+  __shared__ __align__(16) uint16_t tiles[kTileLds];
+  __shared__ __align__(16) uint32_t votes[kVoteWords];
+  const int npairs = w.a.B * w.a.H_kv;
+  WideWork x;
+  if (!wide_work(w, npairs, x)) return;
   bool done;
-  if (kTail != 0 && row_end - row_begin <= kTail)
-    done = attend_cross<kSrc, false, kTail == 192 ? 3 : 2, 1>(a, w.plan, npairs, tiles, votes, pair, split, row_begin, row_end);
+  if (kTail != 0 && x.row_end - x.row_begin <= kTail)
+    done = attend_cross<kSrc, false, kTail == 192 ? 3 : 2, 1>(w.a, w.plan, npairs, tiles, votes, x.pair, x.split, x.row_begin, x.row_end);
   else
-    done = attend_cross<kSrc, false, 2, 2>(a, w.plan, npairs, tiles, votes, pair, split, row_begin, row_end);
+    done = attend_cross<kSrc, false, 2, 2>(w.a, w.plan, npairs, tiles, votes, x.pair, x.split, x.row_begin, x.row_end);
   if (done) return;
   const WideArgs& again = wide_args_again();
 #pragma unroll 1
-  for (uint32_t r = row_begin; r < row_end; r += kWaves * wave_queries(2, 1)) {
+  for (uint32_t r = x.row_begin; r < x.row_end; r += kWaves * wave_queries(2, 1)) {
     __syncthreads();  // the LDS is free
-    attend_cross<kSrc, true, 2, 1>(again.a, again.plan, npairs, tiles, votes, pair, split, r,
-                                   min(row_end, r + (uint32_t)(kWaves * wave_queries(2, 1))));
+    attend_cross<kSrc, true, 2, 1>(again.a, again.plan, npairs, tiles, votes, x.pair, x.split, r,
+                                   min(x.row_end, r + (uint32_t)(kWaves * wave_queries(2, 1))));
   }
+}
+
+// A launch of few workgroups: 128 rows each, eight wavefronts, four for each half of the keys.
+template <int kSrc>
+__global__ __launch_bounds__(2 * kAttnThreads, 2) void cross_halves_kernel(WideArgs w) {
+  __shared__ __align__(16) uint16_t tiles[2 * kTileLds];
+  __shared__ __align__(16) uint32_t votes[kVoteWords];
+  const int npairs = w.a.B * w.a.H_kv;
+  WideWork x;
+  if (!wide_work(w, npairs, x)) return;
+  if (attend_cross<kSrc, false, 2, 1, kSplitKeys>(w.a, w.plan, npairs, tiles, votes, x.pair, x.split, x.row_begin, x.row_end)) return;
+  __syncthreads();
+  const WideArgs& again = wide_args_again();
+  attend_cross<kSrc, true, 2, 1, kTwin>(again.a, again.plan, npairs, tiles, votes, x.pair, x.split, x.row_begin, x.row_end);
 }
 
 // ---------------------------------------------------------------------------
@@ -570,10 +636,11 @@ static void launch_join(const CrossArgs& a, int splits, int64_t pairs, int64_t r
 // the wide kernel reaches a tile's 64 rows with 32-bit byte offsets
 static bool wide_fits(int64_t stride) { return stride <= ((int64_t)1 << 23); }
 
-size_t cross_partial_floats(int64_t B, int64_t NQ, int64_t NK, int64_t H, int64_t H_kv) {
+size_t cross_partial_floats(int64_t B, int64_t NQ, int64_t NK, int64_t H, int64_t H_kv, bool ragged) {
   const int64_t pairs = B * H_kv, rows = NQ * (H / H_kv);
   // a call's strides choose between two plans: enough for either
-  const int a = plan_cross(pairs, rows, NK, true).splits, b = plan_cross(pairs, rows, NK, false).splits, splits = a > b ? a : b;
+  const int a = plan_cross(pairs, rows, NK, ragged, true).splits, b = plan_cross(pairs, rows, NK, ragged, false).splits;
+  const int splits = a > b ? a : b;
   return splits > 1 ? (size_t)splits * pairs * rows * (kHeadDim + 2) : 0;
 }
 
@@ -613,7 +680,8 @@ static hipError_t launch_wide(const CrossArgs& a, const CrossPlan& p, hipStream_
     const dim3 grid((unsigned)tile_list((int)(w.a.B * a.H_kv * p.splits), (int)p.row_tiles).groups);
     const dim3 block(kAttnThreads);
     const int narrow = p.width == 128 ? 128 : p.tail;
-    if (narrow == 0) hipLaunchKernelGGL((cross_wide_kernel<kSrc, 0>), grid, block, 0, st, w);
+    if (p.halves) hipLaunchKernelGGL(cross_halves_kernel<kSrc>, grid, dim3(2 * kAttnThreads), 0, st, w);
+    else if (narrow == 0) hipLaunchKernelGGL((cross_wide_kernel<kSrc, 0>), grid, block, 0, st, w);
     else if (narrow == 192) hipLaunchKernelGGL((cross_wide_kernel<kSrc, 192>), grid, block, 0, st, w);
     else hipLaunchKernelGGL((cross_wide_kernel<kSrc, 128>), grid, block, 0, st, w);
   }
@@ -622,7 +690,7 @@ static hipError_t launch_wide(const CrossArgs& a, const CrossPlan& p, hipStream_
 
 hipError_t launch_cross(const CrossArgs& a, hipStream_t st) {
   const int64_t pairs = (int64_t)a.B * a.H_kv, rows = (int64_t)a.NQ * a.group;
-  const CrossPlan p = plan_cross(pairs, rows, a.NK, a.pages || (wide_fits(a.k_stride) && wide_fits(a.v_stride)));
+  const CrossPlan p = plan_cross(pairs, rows, a.NK, cross_ragged(a.B, a.q_lens, a.k_lens), a.pages || (wide_fits(a.k_stride) && wide_fits(a.v_stride)));
   (void)hipGetLastError();
   if (p.wide) {
     const hipError_t e = a.pages ? launch_wide<kSrcPaged>(a, p, st) : launch_wide<kSrcStrided>(a, p, st);

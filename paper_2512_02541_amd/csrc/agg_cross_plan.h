@@ -12,6 +12,7 @@ struct CrossPlan {
   int tiles;          // few: 16-row tiles of a wavefront
   int width;          // wide: rows of a workgroup, 256 or 128
   int tail;           // wide: rows of a pair's last workgroup where they are fewer, 0: it is as wide as the others
+  int halves;         // wide, of width 128: eight wavefronts, four for each half of a workgroup's keys
   int64_t row_tiles;  // workgroups along a pair's rows
   int splits;         // ... along its keys; more than one: partial results, joined by a second launch
 };
@@ -23,10 +24,10 @@ constexpr int kWideRows = 256;  // rows of a wide workgroup
 constexpr int kMostSplits = 64;
 constexpr int kMostShared = 4096;  // most workgroups of a call that is shared out along the keys
 
-// wide_fits: the distances between rows are what the wide kernel can address
-inline CrossPlan plan_cross(int64_t pairs, int64_t rows, int64_t keys, bool wide_fits) {
+// wide_fits: the distances between rows are what the wide kernel can address; ragged: the sequences may have different lengths
+inline CrossPlan plan_cross(int64_t pairs, int64_t rows, int64_t keys, bool ragged, bool wide_fits) {
   CrossPlan p;
-  p.width = p.tail = 0;
+  p.width = p.tail = p.halves = 0;
   p.tiles = rows <= 16 ? 1 : 2;
   p.row_tiles = (rows + 16 * p.tiles - 1) / (16 * p.tiles);
   // Up to 32 rows the kernel of few rows.  Up to 64 while its two workgroups of a pair all run at once: us, few / wide, paged, 16 heads, 64 queries
@@ -51,25 +52,29 @@ inline CrossPlan plan_cross(int64_t pairs, int64_t rows, int64_t keys, bool wide
   }
   // Width and splits by predicted time: rounds of 512 workgroups (two on a CU; alone on it one takes little more than half as
   // long), each with its start, its end and its share of the key tiles; a second launch and the partial results' way to
-  // memory and back.
+  // memory and back.  Workgroups of 128 rows that all run alone on their CUs have eight wavefronts, four for each half of their keys, where
+  // that is tiles enough.  Of sequences of different lengths half the workgroups are taken to be there.
   const int64_t tiles = (keys + 63) / 64;
   double best = -1;
-  p.width = p.splits = 0;
+  p.splits = 0;
   for (int width = kWideRows; width >= 128; width -= 128) {
     const int64_t row_tiles = (rows + width - 1) / width;
     const int rest = (int)(rows % width);
     const int tail = width == 128 || rest == 0 ? 0 : rest <= 128 ? 128 : rest <= 192 ? 192 : 0;
-    const double pair = width == 128 ? 0.565 : 1.0, alone = width == 128 ? 0.34 : 0.535;
+    const double pair = width == 128 ? 0.565 : 1.0;
     const double saved = tail ? (tail == 128 ? 0.435 : 0.21) / (double)row_tiles : 0.0;  // by narrow last workgroups
     for (int s = 1; s <= kMostSplits && (s == 1 || (tiles / s >= 4 && pairs * row_tiles * s <= kMostShared)); ++s) {
-      const int64_t groups = pairs * row_tiles * s, rest_groups = groups % 512;
-      const double rounds = (double)(groups / 512) * pair + (rest_groups == 0 ? 0.0 : rest_groups <= 256 ? alone : pair);
-      double us = rounds * (groups > 512 ? 1.0 - saved : 1.0) * (5.0 + 1.65 * (double)((tiles + s - 1) / s));
-      if (s > 1) us += 4.0 + (double)pairs * (double)rows * s * 66 * 8 / 4.4e6;
+      const int64_t groups = pairs * row_tiles * s, there = ragged ? (groups + 1) / 2 : groups, rest_groups = there % 512;
+      const int halves = width == 128 && groups <= 256 && tiles / s >= 8;
+      const double alone = halves ? 0.285 : width == 128 ? 0.34 : 0.535;
+      const double rounds = (double)(there / 512) * pair + (rest_groups == 0 ? 0.0 : rest_groups <= 256 ? alone : pair);
+      double us = rounds * (there > 512 ? 1.0 - saved : 1.0) * 1.65 * (double)((tiles + s - 1) / s) + 4.0 + halves;
+      if (s > 1) us += 6.0 + (double)pairs * (double)rows * s * 66 * 8 / 4.4e6;
       if (best < 0 || us < best) {
         best = us;
         p.width = width;
         p.tail = tail;
+        p.halves = halves;
         p.row_tiles = row_tiles;
         p.splits = s;
       }

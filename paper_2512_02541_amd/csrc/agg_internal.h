@@ -240,8 +240,10 @@ struct CrossArgs {
   float* lse;
   float* partial;  // workspace
 };
+// whether the sequences of a call may have different lengths
+inline bool cross_ragged(int32_t B, const int32_t* q_lens, const int32_t* k_lens) { return B > 1 && (q_lens || k_lens); }
 // floats of workspace
-size_t cross_partial_floats(int64_t B, int64_t NQ, int64_t NK, int64_t H, int64_t H_kv);
+size_t cross_partial_floats(int64_t B, int64_t NQ, int64_t NK, int64_t H, int64_t H_kv, bool ragged);
 hipError_t launch_cross(const CrossArgs& args, hipStream_t st);
 
 // New tokens of a cache (agg_cache_append).

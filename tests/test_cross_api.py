@@ -204,10 +204,10 @@ DRIVER = r"""
 #include "agg_cross_plan.h"
 int main() {
   long long pairs, rows, keys;
-  int fits;
-  while (scanf("%lld %lld %lld %d", &pairs, &rows, &keys, &fits) == 4) {
-    const agg::CrossPlan p = agg::plan_cross(pairs, rows, keys, fits);
-    printf("%d %d %lld %d\n", p.wide ? p.width / 16 : p.tiles, p.tail, (long long)p.row_tiles, p.splits);
+  int ragged, fits;
+  while (scanf("%lld %lld %lld %d %d", &pairs, &rows, &keys, &ragged, &fits) == 5) {
+    const agg::CrossPlan p = agg::plan_cross(pairs, rows, keys, ragged, fits);
+    printf("%d %d %d %lld %d\n", p.wide ? p.width : 16 * p.tiles, p.tail, p.halves, (long long)p.row_tiles, p.splits);
   }
 }
 """
@@ -221,7 +221,7 @@ def plan(tmp_path_factory):
                            "-o", str(d / "plan"), str(d / "plan.cpp")])
 
     def ask(sizes):
-        text = "".join("%d %d %d %d\n" % s for s in sizes)
+        text = "".join("%d %d %d %d %d\n" % s for s in sizes)
         out = subprocess.run([str(d / "plan")], input=text, text=True, check=True, stdout=subprocess.PIPE).stdout
         return [tuple(int(x) for x in line.split()) for line in out.splitlines()]
 
@@ -229,21 +229,34 @@ def plan(tmp_path_factory):
 
 
 def test_every_row_has_a_workgroup_and_every_split_keys(plan):
-    sizes = [(pairs, rows, keys, fits) for pairs in (1, 3, 16, 100, 4096, 2 ** 31 - 1)
+    sizes = [(pairs, rows, keys, ragged, fits) for pairs in (1, 3, 16, 100, 4096, 2 ** 31 - 1)
              for rows in (1, 16, 17, 33, 64, 65, 257, 400, 1374, 10992, 2 ** 30)
-             for keys in (0, 1, 31, 64, 1000, 20000, 137400, 2 ** 31 - 600) for fits in (0, 1)]
-    for (pairs, rows, keys, fits), (tiles, tail, row_tiles, splits) in zip(sizes, plan(sizes)):
-        assert row_tiles * 16 * tiles >= rows > (row_tiles - 1) * 16 * tiles
-        assert tiles in (1, 2, 8, 16) and (fits or tiles < 8)
-        assert (tiles >= 8) == (fits and rows > 64 or fits and rows > 32 and pairs * 2 > 256)
-        assert tail in (0, 128, 192) and (tail == 0 or (tiles == 16 and 0 < rows % 256 <= tail))
-        assert 1 <= splits <= max(1, keys // 32) and splits <= 512
+             for keys in (0, 1, 31, 64, 1000, 20000, 137400, 2 ** 31 - 600) for ragged in (0, 1) for fits in (0, 1)]
+    for (pairs, rows, keys, _, fits), (width, tail, halves, row_tiles, splits) in zip(sizes, plan(sizes)):
+        assert row_tiles * width >= rows > (row_tiles - 1) * width
+        assert width in (16, 32, 128, 256) and (fits or width < 128)
+        assert (width >= 128) == (fits and (rows > 64 or rows > 32 and pairs * 2 > 256))
+        assert tail in (0, 128, 192) and (tail == 0 or (width == 256 and 0 < rows % 256 <= tail))
+        assert not halves or (width == 128 and pairs * row_tiles * splits <= 256)
+        assert 1 <= splits <= 64 and (splits == 1 or keys // splits >= (192 if width >= 128 else 1))
 
 
 def test_parts_of_a_batch_share_out_no_keys(plan):
     """More workgroups than a launch takes: no splits, whose partial results a launch of its own could not find."""
-    sizes = [(pairs, rows, 2 ** 31 - 600, 1) for pairs in (2 ** 22, 2 ** 23 + 5, 2 ** 31 - 1) for rows in (65, 256, 1000)]
-    assert all(splits == 1 for _, _, _, splits in plan(sizes))
+    sizes = [(pairs, rows, 2 ** 31 - 600, ragged, 1) for pairs in (2 ** 22, 2 ** 23 + 5, 2 ** 31 - 1) for rows in (65, 256, 1000)
+             for ragged in (0, 1)]
+    assert all(p[-1] == 1 for p in plan(sizes))
+
+
+def test_sizes_reach_their_kernels(plan):
+    """The GPU tests' sizes run every kernel, with and without shared out keys."""
+    import test_gpu_cross as gpu
+
+    asked = [(B * 2, NQ, NK, 0, 1) for B, NQ, NK in gpu.LENGTHS] + [(B * Hk, NQ * (H // Hk), NK, 0, 1) for B, NQ, NK, H, Hk in gpu.WIDE]
+    reached = {(width, tail, halves, splits > 1) for width, tail, halves, _, splits in plan(asked)}
+    for kernel in [(16, 0, 0), (32, 0, 0), (128, 0, 0), (256, 0, 0), (256, 128, 0)]:
+        assert kernel + (False,) in reached and kernel + (True,) in reached, kernel
+    assert (256, 192, 0, False) in reached and (128, 0, 1, False) in reached and (128, 0, 1, True) in reached
 
 
 # ---- the code that is built ----------------------------------------------------------------------------
@@ -285,7 +298,7 @@ def metadata(text, kernels):
 def test_kernels_do_not_spill(assembly):
     """The wide kernels hold two paths' code: nothing of the second may lie in scratch memory while the first runs."""
     found = list(metadata(assembly, r"cross_\w+_kernel"))
-    assert len(found) >= 12 and not [x for x in found if any(x[1].values())]
+    assert len(found) >= 14 and not [x for x in found if any(x[1].values())]
 
 
 def test_append_kernels_do_not_spill(tmp_path):
