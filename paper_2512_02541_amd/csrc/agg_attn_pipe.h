@@ -121,40 +121,46 @@ struct Wave {
   f32x4 S[kQB][2 * kJ];    // [qb][kJ kt + j]: score tiles in flight; key = row_key(4 G + r) + 8 kt
   f32x4 L[kQB][kJ];        // [qb][j]: fast path: element 0 of the lanes G = 0 is the row sum, kept by the matrix core
   float la[kQB][kJ];       // [qb][j]: general path: this lane's part of the row sum
-  float mref[kQB][kJ];     // general path: the row's reference (base-2 logit)
+  float mref[kQB][kJ];     // general path: the row's reference (base-2 logit; exact_logits: plain product)
   Frag a[4];               // [2 kt + h]: K fragments of the block whose scores are being computed
   Frag v[4];               // [dt]: V fragments of the block whose P V is being accumulated
   Frag P[kJ];              // [j]: probabilities of the previous unit
+  float l2;                // exact_logits: scale*log2(e)
   Frag ones;               // A operand of the row sums: row 0 ones, the others zeros
 };
 
 // Probabilities of the 8 kJ base-2 logits a lane holds for a unit, packed as the B operands of
 // the PV MFMAs: for query tile j, contraction elements 8 G .. 8 G + 7 are key tile 0's rows, then
 // key tile 1's.  The query tiles alternate in the instruction stream.
-template <int kJ>
-__device__ __forceinline__ void exp_unit(const f32x4 (&S)[2 * kJ], Frag (&P)[kJ]) {
+// kScaled: the scores are plain products and take the factor l2 = scale*log2(e) here (exact_logits).
+template <int kJ, bool kScaled = false>
+__device__ __forceinline__ void exp_unit(const f32x4 (&S)[2 * kJ], Frag (&P)[kJ], float l2 = 1.f) {
 #pragma unroll
   for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int j = 0; j < kJ; ++j)
-        P[j].u[2 * kt + i] = pack_bf16(fast_exp2(S[kJ * kt + j][2 * i]), fast_exp2(S[kJ * kt + j][2 * i + 1]));
+        {
+          const float s0 = S[kJ * kt + j][2 * i], s1 = S[kJ * kt + j][2 * i + 1];
+          P[j].u[2 * kt + i] = pack_bf16(fast_exp2(kScaled ? s0 * l2 : s0), fast_exp2(kScaled ? s1 * l2 : s1));
+        }
 }
 
 // General path: the same, and the sums of each query tile's part (there the vector ALU keeps
 // the sums: the unit's own sum is what tells that a score has run away from the row's reference,
 // and it is needed before the probabilities reach the matrix core)
-template <int kJ>
-__device__ __forceinline__ void exp_unit_sum(const f32x4 (&S)[2 * kJ], Frag (&P)[kJ], float (&l)[kJ]) {
+template <int kJ, bool kScaled = false>
+__device__ __forceinline__ void exp_unit_sum(const f32x4 (&S)[2 * kJ], Frag (&P)[kJ], float (&l)[kJ], float l2 = 1.f) {
 #pragma unroll
   for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int j = 0; j < kJ; ++j) {
-        const float e0 = fast_exp2(S[kJ * kt + j][2 * i]);
-        const float e1 = fast_exp2(S[kJ * kt + j][2 * i + 1]);
+        const float s0 = S[kJ * kt + j][2 * i], s1 = S[kJ * kt + j][2 * i + 1];
+        const float e0 = fast_exp2(kScaled ? s0 * l2 : s0);
+        const float e1 = fast_exp2(kScaled ? s1 * l2 : s1);
         P[j].u[2 * kt + i] = pack_bf16(e0, e1);
         l[j] += e0;
         l[j] += e1;
@@ -180,6 +186,11 @@ __device__ __forceinline__ void exp_unit_sum(const f32x4 (&S)[2 * kJ], Frag (&P)
 // The last two may end anywhere in memory that holds something else: their values are masked behind the last key, since 0
 // times what lies there may be no number.
 enum { kSrcCompact = 0, kSrcRows = 1, kSrcIndexed = 2, kSrcStrided = 3, kSrcPaged = 4 };
+// Whose scores are products of the query as it is, multiplied by scale*log2(e) in float32 in front of the exponential, rather than
+// of the query times that rounded to bf16.  The vector ALU, as loaded as the matrix core without it, has one instruction more
+// per score: 8 frames over 40 1874 -> 2043 us, 24 frames x 512 queries 62.5 -> 66.9, a frame over 13740 keys 81 -> 88; the result's error
+// against 64 bits 0.0033 -> 0.0020 of it, 0.0017 of which are its own rounding.
+constexpr bool exact_logits(int src) { return src == kSrcStrided || src == kSrcPaged; }
 constexpr bool fragment_order(int src) { return src == kSrcCompact || src == kSrcPaged; }
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -528,11 +539,11 @@ __device__ __forceinline__ void tile_steps(Wave<kQB, kJ>& w, const u32x4* __rest
       f32x4 (&S)[2 * kJ] = w.S[qb];
       if (kLast && valid < kTileRows) mask_unit<kJ>(S, kb, valid, G);
       if (!kGen) {
-        exp_unit<kJ>(S, Pn);
+        exp_unit<kJ, exact_logits(kSrc)>(S, Pn, w.l2);
       } else {
         // the scores are already relative to the row's reference; whether it still holds is
         // looked at below, behind the step's last MFMA
-        exp_unit_sum<kJ>(S, Pn, unit_sum);
+        exp_unit_sum<kJ, exact_logits(kSrc)>(S, Pn, unit_sum, w.l2);
       }
     }
     if (do_qk) {
@@ -556,6 +567,8 @@ __device__ __forceinline__ void tile_steps(Wave<kQB, kJ>& w, const u32x4* __rest
       __builtin_amdgcn_sched_group_barrier(0x008, kJ, 0);  // the row-sum products of the last unit
 #pragma unroll
       for (int i = 0; i < 4 * kJ; ++i) {
+        // (orders with the multiplications one by one, behind the MFMAs or all at the end: 0 to 3 % slower)
+        if (exact_logits(kSrc)) __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
         __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);  // transcendental
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // MFMA
         __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
@@ -590,9 +603,9 @@ __device__ __forceinline__ void tile_steps(Wave<kQB, kJ>& w, const u32x4* __rest
             for (int r = 0; r < 4; ++r) mx = fmaxf(mx, S[kJ * kt + j][r]);
           mx = quad_max(mx);  // the four lanes of a row agree
           const float old = w.mref[qb][j];
-          if (mx > kLazy) w.mref[qb][j] = old + mx;
+          if ((exact_logits(kSrc) ? mx * w.l2 : mx) > kLazy) w.mref[qb][j] = old + mx;
           const float d = w.mref[qb][j] - old;
-          const float f = fast_exp2(-d);
+          const float f = fast_exp2(exact_logits(kSrc) ? -d * w.l2 : -d);
 #pragma unroll
           for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -605,7 +618,7 @@ __device__ __forceinline__ void tile_steps(Wave<kQB, kJ>& w, const u32x4* __rest
         }
 #pragma unroll
         for (int j = 0; j < kJ; ++j) unit_sum[j] = 0.f;
-        exp_unit_sum<kJ>(S, w.P, unit_sum);
+        exp_unit_sum<kJ, exact_logits(kSrc)>(S, w.P, unit_sum, w.l2);
       }
 #pragma unroll
       for (int j = 0; j < kJ; ++j) w.la[qb][j] += unit_sum[j];

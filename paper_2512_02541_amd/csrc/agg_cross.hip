@@ -308,6 +308,7 @@ __device__ __forceinline__ bool attend_cross(const CrossArgs& p, const CrossPlan
   }
 
   Wave<kQB, kJ> w;
+  w.l2 = p.scale2;
   const uint32_t one = c == 0 ? 0x3F803F80u : 0u;
   w.ones.u = u32x4{one, one, one, one};
   const uint32_t r_wave = row_begin + wave * kWaveQ;
@@ -324,13 +325,6 @@ __device__ __forceinline__ bool attend_cross(const CrossArgs& p, const CrossPlan
   for (int qb = 0; qb < kQB; ++qb)
 #pragma unroll
     for (int j = 0; j < kJ; ++j) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const u32x4 raw = w.Qf[qb][2 * j + h].u;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          w.Qf[qb][2 * j + h].u[i] = pack_bf16(bf16_lo(raw[i]) * p.scale2, bf16_hi(raw[i]) * p.scale2);
-      }
       // (General path: zeros that the compiler does not know to be zeros.  Knowing them, it spilled 119 to 326 registers of
       // the kernels below, in the narrow ones of the fast path too; a build test checks that none does.)
       float zero = 0.f;
@@ -429,7 +423,7 @@ __device__ __forceinline__ bool attend_cross(const CrossArgs& p, const CrossPlan
         for (int dt = 0; dt < 4; ++dt) *reinterpret_cast<f32x4*>(p.partial + at * kHeadDim + 16 * dt + 4 * eG) = w.O[qb][j][dt];
         if (eG == 0)
           *reinterpret_cast<f32x2*>(partial_sums(p, pairs, plan.splits) + at * 2) =
-              f32x2{kGen ? w.mref[qb][j] : 0.f, l_fin[qb][j]};
+              f32x2{kGen ? w.mref[qb][j] * p.scale2 : 0.f, l_fin[qb][j]};
       }
     return true;
   }
@@ -446,7 +440,7 @@ __device__ __forceinline__ bool attend_cross(const CrossArgs& p, const CrossPlan
         *reinterpret_cast<u32x2*>(epi + (16 * j + ec) * kEpiStride + 16 * dt + 4 * eG) = pack4(w.O[qb][j][dt] * inv);
       if (p.lse && eG == 0 && r0 + 16 * j + ec < row_end) {
         const RowPlace at = row_place(p, hk, r0 + 16 * j + ec);
-        p.lse[((int64_t)b * p.H + at.head) * p.NQ + at.q] = ((kGen ? w.mref[qb][j] : 0.f) + log2f(l)) * kLn2;
+        p.lse[((int64_t)b * p.H + at.head) * p.NQ + at.q] = ((kGen ? w.mref[qb][j] * p.scale2 : 0.f) + log2f(l)) * kLn2;
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
