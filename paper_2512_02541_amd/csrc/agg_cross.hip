@@ -503,8 +503,8 @@ __device__ __forceinline__ bool wide_work(const WideArgs& w, int npairs, WideWor
   // the workgroups of a pair's split read the same keys: on one XCD they share them through its L2
   int unit, i;
   if (!list_tile(tile_list(npairs * w.plan.splits, (int)w.plan.row_tiles), npairs * w.plan.splits, blockIdx.x, unit, i)) return false;
-  x.pair = unit % npairs;
-  x.split = unit / npairs;
+  x.pair = unit / w.plan.splits;  // a long sequence's splits go to different XCDs
+  x.split = unit % w.plan.splits;
   const int b = x.pair / a.H_kv;
   const uint32_t rows = (uint32_t)cross_queries(a, b) * (uint32_t)a.group;
   x.row_begin = (uint32_t)i * (uint32_t)w.plan.width;

@@ -34,15 +34,18 @@ inline CrossPlan plan_cross(int64_t pairs, int64_t rows, int64_t keys, bool ragg
   // to 262 keys 5.4 / 6.7, to 5496 12.6 / 19.4, to 137400 106 / 105; with 384 pairs to 1374 keys 45.7 / 26.1.
   p.wide = wide_fits && rows > kFewRows && (rows > 2 * kFewRows || pairs * p.row_tiles > 256);
   if (!p.wide) {
-    // Splits by predicted time: a start, a wavefront's steps one after another, and a second launch.  More workgroups than run at once
-    // (two on a CU of up to 16 rows, one of more) gain nothing: the memory is busy with them.
+    // Splits by predicted time: a wavefront's steps one after another, and a second launch.  More workgroups than run at once
+    // (two on a CU of up to 16 rows, one of more) gain nothing where the sequences are alike: the memory is busy with them.  Where they
+    // are not, the long ones would end alone: there more rounds are taken, of 1.2 us each (us, one token each over up to 10000 keys of 24
+    // sequences, 16 heads: 124 unsplit, 103 / 95 / 91 / 106 with 2 / 4 / 16 / 32 splits).
     const int64_t groups = pairs * p.row_tiles, steps = (keys + kKeyBlock * kFewWaves - 1) / (kKeyBlock * kFewWaves);
-    const int64_t at_once = p.tiles == 1 ? 512 : 256;
+    const int64_t at_once = p.tiles == 1 ? 512 : 256, most = !ragged ? at_once : p.tiles == 1 ? 4096 : 512;
     const double step = p.tiles == 1 ? 0.55 : 0.85;
     double best = 0;
     p.splits = 1;
-    for (int64_t s = 1; s <= kMostSplits && (s == 1 || (groups * s <= at_once && steps / s >= 1)); ++s) {
-      const double us = (double)((steps + s - 1) / s) * step + (s > 1 ? 3.0 + 0.03 * s : 0.0);
+    for (int64_t s = 1; s <= kMostSplits && (s == 1 || (groups * s <= most && steps / s >= 1)); ++s) {
+      const double us = (double)((steps + s - 1) / s) * step + (s > 1 ? 3.0 + 0.03 * s : 0.0) +
+                        (ragged ? 1.2 * (double)(groups * s) / (double)at_once : 0.0);
       if (s == 1 || us < best) {
         best = us;
         p.splits = (int)s;
@@ -50,26 +53,34 @@ inline CrossPlan plan_cross(int64_t pairs, int64_t rows, int64_t keys, bool ragg
     }
     return p;
   }
-  // Width and splits by predicted time: rounds of 512 workgroups (two on a CU; alone on it one takes little more than half as
-  // long), each with its start, its end and its share of the key tiles; a second launch and the partial results' way to
-  // memory and back.  Workgroups of 128 rows that all run alone on their CUs have eight wavefronts, four for each half of their keys, where
-  // that is tiles enough.  Of sequences of different lengths half the workgroups are taken to be there.
+  // Width and splits by predicted time.  A tile of keys takes 256 rows 1.65 us, two workgroups on a CU, and 0.535 of that alone on it;
+  // 128 rows 0.565 and 0.34 of it; 128 rows and eight wavefronts, four for each half of the keys, 0.285, always alone.  To that come
+  // starts and ends, and for splits a second launch and the partial results' way to memory and back.
+  // Like sequences: rounds of as many workgroups as run at once, eight wavefronts where that is one round.  Sequences of different
+  // lengths: 0.4 of the work is taken to be there, and a longest piece behind it (fitted to eight such calls, of which
+  // it takes what is 0 to 10 % off the fastest).
   const int64_t tiles = (keys + 63) / 64;
   double best = -1;
   p.splits = 0;
-  for (int width = kWideRows; width >= 128; width -= 128) {
-    const int64_t row_tiles = (rows + width - 1) / width;
+  for (int kind = 0; kind < 3; ++kind) {
+    const int width = kind == 0 ? kWideRows : 128, halves = kind == 2;
+    const int64_t row_tiles = (rows + width - 1) / width, at_once = halves ? 256 : 512;
     const int rest = (int)(rows % width);
     const int tail = width == 128 || rest == 0 ? 0 : rest <= 128 ? 128 : rest <= 192 ? 192 : 0;
-    const double pair = width == 128 ? 0.565 : 1.0;
+    const double pair = (halves ? 0.285 : width == 128 ? 0.565 : 1.0) * 1.65, alone = (halves ? 0.285 : width == 128 ? 0.34 : 0.535) * 1.65;
     const double saved = tail ? (tail == 128 ? 0.435 : 0.21) / (double)row_tiles : 0.0;  // by narrow last workgroups
     for (int s = 1; s <= kMostSplits && (s == 1 || (tiles / s >= 4 && pairs * row_tiles * s <= kMostShared)); ++s) {
-      const int64_t groups = pairs * row_tiles * s, there = ragged ? (groups + 1) / 2 : groups, rest_groups = there % 512;
-      const int halves = width == 128 && groups <= 256 && tiles / s >= 8;
-      const double alone = halves ? 0.285 : width == 128 ? 0.34 : 0.535;
-      const double rounds = (double)(there / 512) * pair + (rest_groups == 0 ? 0.0 : rest_groups <= 256 ? alone : pair);
-      double us = rounds * (there > 512 ? 1.0 - saved : 1.0) * 1.65 * (double)((tiles + s - 1) / s) + 4.0 + halves;
-      if (s > 1) us += 6.0 + (double)pairs * (double)rows * s * 66 * 8 / 4.4e6;
+      const int64_t groups = pairs * row_tiles * s, last = groups % at_once;
+      if (halves && (tiles / s < 8 || (!ragged && groups > at_once))) continue;
+      const double here = (double)((tiles + s - 1) / s);
+      double us, join = s > 1 ? 6.0 + (double)pairs * (double)rows * s * 66 * 8 / 4.4e6 * (ragged ? 0.4 : 1.0) : 0.0;
+      if (ragged) {
+        const double ends = width == 128 ? 5.0 : 8.0;
+        us = 0.4 * (double)groups / (double)at_once * (pair * here + ends) + alone * here + ends + join;
+      } else {
+        const double rounds = (double)(groups / at_once) * pair + (last == 0 ? 0.0 : last <= 256 ? alone : pair);
+        us = rounds * (groups > at_once ? 1.0 - saved : 1.0) * here + 4.0 + halves + join;
+      }
       if (best < 0 || us < best) {
         best = us;
         p.width = width;

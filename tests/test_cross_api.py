@@ -232,12 +232,12 @@ def test_every_row_has_a_workgroup_and_every_split_keys(plan):
     sizes = [(pairs, rows, keys, ragged, fits) for pairs in (1, 3, 16, 100, 4096, 2 ** 31 - 1)
              for rows in (1, 16, 17, 33, 64, 65, 257, 400, 1374, 10992, 2 ** 30)
              for keys in (0, 1, 31, 64, 1000, 20000, 137400, 2 ** 31 - 600) for ragged in (0, 1) for fits in (0, 1)]
-    for (pairs, rows, keys, _, fits), (width, tail, halves, row_tiles, splits) in zip(sizes, plan(sizes)):
+    for (pairs, rows, keys, ragged, fits), (width, tail, halves, row_tiles, splits) in zip(sizes, plan(sizes)):
         assert row_tiles * width >= rows > (row_tiles - 1) * width
         assert width in (16, 32, 128, 256) and (fits or width < 128)
         assert (width >= 128) == (fits and (rows > 64 or rows > 32 and pairs * 2 > 256))
         assert tail in (0, 128, 192) and (tail == 0 or (width == 256 and 0 < rows % 256 <= tail))
-        assert not halves or (width == 128 and pairs * row_tiles * splits <= 256)
+        assert not halves or (width == 128 and (ragged or pairs * row_tiles * splits <= 256))
         assert 1 <= splits <= 64 and (splits == 1 or keys // splits >= (192 if width >= 128 else 1))
 
 

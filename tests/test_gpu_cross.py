@@ -118,7 +118,8 @@ def test_lengths(B, NQ, NK):
 
 # sizes that fill the card with workgroups of 256 rows: B, NQ, NK, H, H_kv
 WIDE = [(20, 512, 90, 16, 16), (24, 512, 400, 16, 16), (20, 520, 130, 16, 16), (20, 440, 100, 16, 16), (16, 190, 65, 32, 16), (1, 1374, 9000, 16, 16),
-        (2, 700, 6000, 16, 8), (1, 2816, 8000, 16, 16), (6, 128, 700, 4, 4), (3, 500, 1500, 16, 4), (2, 1024, 12000, 16, 16)]
+        (2, 700, 6000, 16, 8), (1, 2816, 8000, 16, 16), (6, 128, 700, 4, 4), (3, 500, 1500, 16, 4), (2, 1024, 12000, 16, 16),
+        (1, 600, 20000, 2, 2), (3, 380, 9000, 1, 1)]
 
 
 @pytest.mark.parametrize("B, NQ, NK, H, H_kv", WIDE)
