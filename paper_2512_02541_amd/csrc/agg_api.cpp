@@ -584,6 +584,7 @@ int check_cross(const agg_cross* c) {
   if (c->D != kHeadDim) return AGG_ERR_UNSUPPORTED;
   // rows of a key head and key numbers are counted with 31 bits, a tensor stays under 2^60 bytes
   constexpr int64_t kMost = INT32_MAX - 512;
+  if (c->H > (1 << 22)) return AGG_ERR_OVERFLOW;  // a token's channels are counted with 31 bits
   if (c->NK > kMost || (int64_t)c->NQ * (c->H / c->H_kv) > kMost || (int64_t)c->B * c->H > INT32_MAX) return AGG_ERR_OVERFLOW;
   const int64_t longest = c->NQ > c->NK ? c->NQ : c->NK;
   if (longest > 0 && (int64_t)c->B * c->H > ((int64_t)1 << 40) / longest) return AGG_ERR_OVERFLOW;
@@ -595,7 +596,7 @@ int check_cache(const agg_cache* c) {
   if (c->n_pages < 1 || c->H < 1 || c->D < 1 || c->B < 1 || c->max_pages < 1) return AGG_ERR_SHAPE;
   if (c->D != kHeadDim) return AGG_ERR_UNSUPPORTED;
   // rows of a sequence are counted with 31 bits, a pool stays under 2^60 bytes
-  if (c->max_pages > (INT32_MAX - 512) / kTileRows || (int64_t)c->n_pages * c->H > ((int64_t)1 << 46)) return AGG_ERR_OVERFLOW;
+  if (c->H > (1 << 22) || c->max_pages > (INT32_MAX - 512) / kTileRows || (int64_t)c->n_pages * c->H > ((int64_t)1 << 46)) return AGG_ERR_OVERFLOW;
   return AGG_OK;
 }
 uint64_t pool_bytes(const agg_cache* c) { return (uint64_t)c->n_pages * c->H * kTileElems * 2; }

@@ -36,7 +36,7 @@ inline CrossPlan plan_cross(int64_t pairs, int64_t rows, int64_t keys, bool ragg
   if (!p.wide) {
     // Splits by predicted time: a wavefront's steps one after another, and a second launch.  More workgroups than run at once
     // (two on a CU of up to 16 rows, one of more) gain nothing where the sequences are alike: the memory is busy with them.  Where they
-    // are not, the long ones would end alone: there more rounds are taken, of 1.2 us each (us, one token each over up to 10000 keys of 24
+    // are not, the long ones would end alone: there more rounds are taken, of 2 us each (us, one token each over up to 10000 keys of 24
     // sequences, 16 heads: 124 unsplit, 103 / 95 / 91 / 106 with 2 / 4 / 16 / 32 splits).
     const int64_t groups = pairs * p.row_tiles, steps = (keys + kKeyBlock * kFewWaves - 1) / (kKeyBlock * kFewWaves);
     const int64_t at_once = p.tiles == 1 ? 512 : 256, most = !ragged ? at_once : p.tiles == 1 ? 4096 : 512;
@@ -45,7 +45,7 @@ inline CrossPlan plan_cross(int64_t pairs, int64_t rows, int64_t keys, bool ragg
     p.splits = 1;
     for (int64_t s = 1; s <= kMostSplits && (s == 1 || (groups * s <= most && steps / s >= 1)); ++s) {
       const double us = (double)((steps + s - 1) / s) * step + (s > 1 ? 3.0 + 0.03 * s : 0.0) +
-                        (ragged ? 1.2 * (double)(groups * s) / (double)at_once : 0.0);
+                        (ragged ? 2.0 * (double)(groups * s) / (double)at_once : 0.0);
       if (s == 1 || us < best) {
         best = us;
         p.splits = (int)s;

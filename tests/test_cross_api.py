@@ -102,7 +102,7 @@ def test_cross_refusals():
         assert _cross(**bad) == S, bad
     assert _cross(qs=1 << 57) == O and _cross(ks=1 << 56) == O and _cross(vs=1 << 56) == O
     assert _cross(NK=2 ** 31 - 1) == O and _cross(NQ=2 ** 30, H=4, H_kv=1) == O and _cross(B=2 ** 30) == O
-    assert _cross(B=2 ** 20, NK=2 ** 30, H=2) == O
+    assert _cross(B=2 ** 20, NK=2 ** 30, H=2) == O and _cross(H=2 ** 22 + 2) == O and _cached(H=2 ** 22 + 1) == O
     # split keys need a workspace
     c = dict(B=1, NQ=1, NK=100000, H=4, H_kv=4)
     need = agg.agg_cross_workspace_bytes(agg.make_cross(1, 1, 100000, 4))
