@@ -257,6 +257,9 @@ def test_sizes_reach_their_kernels(plan):
     for kernel in [(16, 0, 0), (32, 0, 0), (128, 0, 0), (256, 0, 0), (256, 128, 0)]:
         assert kernel + (False,) in reached and kernel + (True,) in reached, kernel
     assert (256, 192, 0, False) in reached and (128, 0, 1, False) in reached and (128, 0, 1, True) in reached
+    redone = {(width, tail, halves, splits > 1)
+              for width, tail, halves, _, splits in plan([(B * H, NQ, NK, 0, 1) for B, NQ, NK, H in gpu.REDO])}
+    assert {k for k in reached if k[0] >= 128} == redone
 
 
 # ---- the code that is built ----------------------------------------------------------------------------

@@ -217,6 +217,31 @@ def test_large_logits(NQ, NK):
         check(cross, harness.cross_forward(cross, q2, k2, v), q2, k2, v, what="shifted %d" % sign)
 
 
+# a size for each wide kernel, with and without shared out keys: B, NQ, NK, H
+REDO = [(20, 440, 100, 16), (24, 512, 400, 16), (20, 520, 130, 16), (1, 1374, 9000, 16), (1, 2816, 8000, 16), (1, 777, 1029, 2),
+        (1, 600, 20000, 2), (1, 90, 5000, 2), (2, 130, 200, 2)]
+
+
+@pytest.mark.parametrize("B, NQ, NK, H", REDO)
+def test_rows_redone_on_every_route(B, NQ, NK, H):
+    """Logits that leave the fast path's range in one workgroup, and in all, early and late among the keys."""
+    say("redone", B, NQ, NK, H)
+    g = gen(13)
+    q, k, v = bf16(g, B, NQ, H, 64), bf16(g, B, NK, H, 64, scale=0.5), bf16(g, B, NK, H, 64)
+    u = torch.sign(torch.randn(64, generator=g, device="cuda"))
+    cross = agg.make_cross(B, NQ, NK, H)
+    for rows, at in ((slice(NQ - 1, NQ), 3), (slice(0, NQ, 50), NK - 2)):
+        q2, k2 = q.clone(), k.clone()
+        q2[:, rows] = (6 * u).to(torch.bfloat16)  # logit 6 * 6 * 64 / 8 = 288 with that key, -288 with its neighbour
+        k2[:, at] = (6 * u).to(torch.bfloat16)
+        k2[:, at + 1] = (-6 * u).to(torch.bfloat16)
+        check(cross, harness.cross_forward(cross, q2, k2, v), q2, k2, v, what="rows %s key %d" % (rows, at))
+        pages, n = pages_of(g, B, -(-NK // 64))
+        pools = harness.make_pools(n, H, "cuda")
+        put(pools, pages, k2, v)
+        check(cross, harness.cache_forward(agg.make_cache(*pools, pages, H), cross, q2), q2, k2, v, what="cached, key %d" % at)
+
+
 @pytest.mark.parametrize("NQ", [3, 50, 300])
 def test_rows_that_are_no_numbers(NQ):
     """A query that is NaN spoils its own row, a key that is NaN its sequence, a value that is NaN its channel."""
