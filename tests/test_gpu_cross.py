@@ -127,6 +127,12 @@ def test_many_rows(B, NQ, NK, H, H_kv):
     both(B, NQ, NK, H, H_kv, seed=12)
 
 
+@pytest.mark.parametrize("B, NQ, NK, H, H_kv", [(64, 3, 70, 12, 12), (61, 20, 40, 13, 13), (257, 1, 33, 3, 3), (100, 33, 65, 4, 4)])
+def test_many_pairs(B, NQ, NK, H, H_kv):
+    """Workgroups of few rows dealt out to the XCDs in runs, as many as eight of them hold and some more or fewer."""
+    both(B, NQ, NK, H, H_kv, seed=14)
+
+
 @pytest.mark.parametrize("NQ", [1, 7, 30, 200])
 @pytest.mark.parametrize("H, H_kv", [(1, 1), (4, 4), (12, 4), (16, 1), (33, 33), (20, 5), (6, 2)])
 def test_heads(H, H_kv, NQ):
