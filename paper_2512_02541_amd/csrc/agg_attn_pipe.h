@@ -188,8 +188,8 @@ __device__ __forceinline__ void exp_unit_sum(const f32x4 (&S)[2 * kJ], Frag (&P)
 enum { kSrcCompact = 0, kSrcRows = 1, kSrcIndexed = 2, kSrcStrided = 3, kSrcPaged = 4 };
 // Whose scores are products of the query as it is, multiplied by scale*log2(e) in float32 in front of the exponential, rather than
 // of the query times that rounded to bf16.  The vector ALU, as loaded as the matrix core without it, has one instruction more
-// per score: 8 frames over 40 1874 -> 2043 us, 24 frames x 512 queries 62.5 -> 66.9, a frame over 13740 keys 81 -> 88; the result's error
-// against 64 bits 0.0033 -> 0.0020 of it, 0.0017 of which are its own rounding.
+// per score, 7 to 15 % of a call by box (8 frames over 40 1874 -> 2043 us, 24 frames x 512 queries 62.5 -> 66.9, a frame over 13740 keys
+// 81 -> 88 on one); the result's error against 64 bits is 0.0023 of it instead of 0.0034, 0.0017 of which are its own rounding.
 constexpr bool exact_logits(int src) { return src == kSrcStrided || src == kSrcPaged; }
 constexpr bool fragment_order(int src) { return src == kSrcCompact || src == kSrcPaged; }
 

@@ -10,12 +10,16 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 // ---------------------------------------------------------------------------
-// A workgroup takes 32 consecutive rows of a sequence, half a page, and the tokens that become them: keys, values and queries.
-// It works out their cosines and signed sines once, a pair of channels a thread, and its wavefronts take the heads in turn, eight
-// lanes a row of a head, a head's rows requested while the one before is worked on.  A key's 16-byte chunk goes to the page
-// from the registers it was turned in: eight consecutive rows make a whole 128-byte line of one chunk number.  Values turn
-// through LDS with the transposing read, which leaves a lane with the eight rows of one channel that make a chunk of the
+// A workgroup takes 32 (few rows: 16) consecutive rows of a sequence, half or a quarter of a page, and the tokens that become them:
+// keys, values and queries.  It works out their cosines and signed sines once, a pair of channels a thread, and its wavefronts take
+// the heads in turn, eight lanes a row of a head, a head's rows requested while the one before is worked on.  A key's 16-byte chunk
+// goes to the page from the registers it was turned in: eight consecutive rows make a whole 128-byte line of one chunk number.
+// Values turn through LDS with the transposing read, which leaves a lane with the eight rows of one channel that make a chunk of the
 // page; a chunk that the new rows fill only in part is stored element by element, so that its other rows stay.
+// Many rows are bound by HBM: 137400 of 16 heads, keys and values, 225 us = 5.0 TB/s; 21984 with their queries 57 us.  Few are one
+// chain of latencies (lengths, page, rows, sines, exchange): a frame of 1374 tokens 7.8 to 8.8 us (12 in pieces of 32), one token
+// 4.9.  Partners fetched through LDS took 21984 rows 68 us, with eight-way bank conflicts; queries and keys in workgroups of
+// their own, each with a table, 3 x 8328 tokens of 12 and 4 heads 41 us instead of 30.
 // ---------------------------------------------------------------------------
 constexpr int kAppendThreads = 256;
 constexpr int kAppendWaves = kAppendThreads / 64;
@@ -32,9 +36,8 @@ struct Channels {
   int lane_at;          // kPairsAcrossLanes: 4 * the lane that holds the others
 };
 
-// orders this wavefront's LDS writes before its later reads, and its earlier reads before its later writes
-// (wave_lds_fence); a row's table of cosines and signed sines: 16-byte chunk q of lane j (channels 8 j + 2 q, + 1) at this place,
-// so that the sixteen lanes served together, of two rows, read from different banks
+// a row's table of cosines and signed sines: 16-byte chunk q of lane j (channels 8 j + 2 q, + 1) lies at this place, so that the
+// sixteen lanes served together, of two rows, read from different banks
 __device__ __forceinline__ int turn_chunk(int row, int q, int j) { return row * 32 + ((q * 8 + j) ^ (8 * (row & 1))); }
 
 // norm of a row's eight channels.  affine: what the norm multiplies by (from the lane's first channel on) and, kHeadDim behind, adds
