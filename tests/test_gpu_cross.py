@@ -478,8 +478,9 @@ def test_append_given_positions_and_parts_left_out():
                                            (agg.AGG_ROPE_SECTIONS, (20, 22, 14)), (agg.AGG_ROPE_HEAD, (0, 0, 0))])
 def test_append_many_rows(pairing, axes):
     """More rows than pieces of 16 take: pieces of 32, beginning and ending inside one."""
+    append_case(frames(3, 9, 37, 37, 5, 7), 7, [5, 49, 64], [12366, 5401, 9000], pairing=pairing, axes=axes, strided=True)
+    append_case(frames(5, 8, 37, 37, 5, 6), 6, [1, 31, 4000, 0, 77], None, pairing=pairing, axes=axes, kind="rms", max_pages=200, queries=axes[1] != 24)
     append_case(frames(3, 2, 37, 37, 5, 3), 3, [5, 49, 64], [2748, 1401, 2000], pairing=pairing, axes=axes, strided=True)
-    append_case(frames(3, 3, 37, 37, 5, 6), 2, [1, 31, 4000], None, pairing=pairing, axes=axes, kind="rms", max_pages=100, queries=axes[1] != 24)
 
 
 def test_append_a_frame():
