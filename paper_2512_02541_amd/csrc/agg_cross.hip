@@ -651,9 +651,12 @@ static bool wide_fits(int64_t stride) { return stride <= ((int64_t)1 << 23); }
 
 size_t cross_partial_floats(int64_t B, int64_t NQ, int64_t NK, int64_t H, int64_t H_kv, bool ragged) {
   const int64_t pairs = B * H_kv, rows = NQ * (H / H_kv);
-  // a call's strides choose between two plans: enough for either
-  const int a = plan_cross(pairs, rows, NK, ragged, true).splits, b = plan_cross(pairs, rows, NK, ragged, false).splits;
-  const int splits = a > b ? a : b;
+  // where a call's keys lie chooses between three plans: enough for any
+  int splits = plan_cross(pairs, rows, NK, ragged, true, true).splits;
+  for (bool fits : {true, false}) {
+    const int s = plan_cross(pairs, rows, NK, ragged, fits, false).splits;
+    splits = s > splits ? s : splits;
+  }
   return splits > 1 ? (size_t)splits * pairs * rows * (kHeadDim + 2) : 0;
 }
 
@@ -706,7 +709,8 @@ static hipError_t launch_wide(const CrossArgs& a, const CrossPlan& p, hipStream_
 
 hipError_t launch_cross(const CrossArgs& a, hipStream_t st) {
   const int64_t pairs = (int64_t)a.B * a.H_kv, rows = (int64_t)a.NQ * a.group;
-  const CrossPlan p = plan_cross(pairs, rows, a.NK, cross_ragged(a.B, a.q_lens, a.k_lens), a.pages || (wide_fits(a.k_stride) && wide_fits(a.v_stride)));
+  const CrossPlan p = plan_cross(pairs, rows, a.NK, cross_ragged(a.B, a.q_lens, a.k_lens),
+                                 a.pages || (wide_fits(a.k_stride) && wide_fits(a.v_stride)), a.pages != nullptr);
   (void)hipGetLastError();
   const hipError_t e = p.wide ? a.pages ? launch_wide<kSrcPaged>(a, p, st) : launch_wide<kSrcStrided>(a, p, st)
                        : a.pages ? launch_few<true>(a, p, pairs, st) : launch_few<false>(a, p, pairs, st);

@@ -24,16 +24,14 @@ constexpr int kWideRows = 256;  // rows of a wide workgroup
 constexpr int kMostSplits = 64;
 constexpr int kMostShared = 4096;  // most workgroups of a call that is shared out along the keys
 
-// wide_fits: the distances between rows are what the wide kernel can address; ragged: the sequences may have different lengths
-inline CrossPlan plan_cross(int64_t pairs, int64_t rows, int64_t keys, bool ragged, bool wide_fits) {
+// wide_fits: the distances between rows are what the wide kernel can address; ragged: the sequences may have different lengths;
+// paged: keys and values in a cache
+inline CrossPlan plan_cross(int64_t pairs, int64_t rows, int64_t keys, bool ragged, bool wide_fits, bool paged) {
   CrossPlan p;
-  p.width = p.tail = p.halves = 0;
+  p.wide = p.width = p.tail = p.halves = 0;
   p.tiles = rows <= 16 ? 1 : 2;
   p.row_tiles = (rows + 16 * p.tiles - 1) / (16 * p.tiles);
-  // Up to 32 rows the kernel of few rows.  Up to 64 while its two workgroups of a pair all run at once: us, few / wide, paged, 16 heads, 64 queries
-  // to 262 keys 5.4 / 6.7, to 5496 12.6 / 19.4, to 137400 106 / 105; with 384 pairs to 1374 keys 45.7 / 26.1.
-  p.wide = wide_fits && rows > kFewRows && (rows > 2 * kFewRows || pairs * p.row_tiles > 256);
-  if (!p.wide) {
+  if (rows <= kFewRows || !wide_fits) {
     // Splits by predicted time: a wavefront's steps one after another, and a second launch.  More workgroups than run at once
     // (two on a CU of up to 16 rows, one of more) gain nothing where the sequences are alike: the memory is busy with them.  Where they
     // are not, the long ones would end alone: there more rounds are taken, of 2 us each (us, one token each over up to 10000 keys of 24
@@ -53,37 +51,44 @@ inline CrossPlan plan_cross(int64_t pairs, int64_t rows, int64_t keys, bool ragg
     }
     return p;
   }
-  // Width and splits by predicted time.  A tile of keys takes 256 rows 1.65 us, two workgroups on a CU, and 0.535 of that alone on it;
-  // 128 rows 0.565 and 0.34 of it; 128 rows and eight wavefronts, four for each half of the keys, 0.285, always alone.  To that come
-  // starts and ends, and for splits a second launch and the partial results' way to memory and back.
+  // Kernel, width and splits by predicted time.  A tile of keys takes 256 rows 1.65 us, two workgroups on a CU, and 0.535 of that alone on it;
+  // 128 rows 0.565 and 0.34 of it; 128 rows and eight wavefronts, four for each half of the keys, 0.285, always alone; 32 rows of the
+  // kernel of few rows 0.22 us out of pages and 0.33 in place, always alone.  To that come starts and ends, and for splits a second
+  // launch and the partial results' way to memory and back.  (us, few / wide, out of pages, 16 heads: 261 queries to 1374 keys 9.0 / 13.0,
+  // 512 to 512 6.3 / 8.9, 64 to 137400 106 / 105, 64 of 24 sequences to 1374 45.7 / 26.1; in place 261 to 1374 11.9 / 13.3, 522 to 522
+  // 13.8 / 9.6.)
   // Like sequences: rounds of as many workgroups as run at once, eight wavefronts where that is one round.  Sequences of different
   // lengths: 0.4 of the work is taken to be there, and a longest piece behind it (fitted to eight such calls, of which
   // it takes what is 0 to 10 % off the fastest).
   const int64_t tiles = (keys + 63) / 64;
   double best = -1;
   p.splits = 0;
-  for (int kind = 0; kind < 3; ++kind) {
-    const int width = kind == 0 ? kWideRows : 128, halves = kind == 2;
-    const int64_t row_tiles = (rows + width - 1) / width, at_once = halves ? 256 : 512;
+  for (int kind = 0; kind < 4; ++kind) {
+    const int width = kind == 0 ? kWideRows : kind == 3 ? kFewRows : 128, halves = kind == 2, few = kind == 3;
+    const int64_t row_tiles = (rows + width - 1) / width, at_once = halves || few ? 256 : 512;
     const int rest = (int)(rows % width);
-    const int tail = width == 128 || rest == 0 ? 0 : rest <= 128 ? 128 : rest <= 192 ? 192 : 0;
-    const double pair = (halves ? 0.285 : width == 128 ? 0.565 : 1.0) * 1.65, alone = (halves ? 0.285 : width == 128 ? 0.34 : 0.535) * 1.65;
+    const int tail = width != kWideRows || rest == 0 ? 0 : rest <= 128 ? 128 : rest <= 192 ? 192 : 0;
+    const double pair = few ? (paged ? 0.22 : 0.33) : (halves ? 0.285 : width == 128 ? 0.565 : 1.0) * 1.65;
+    const double alone = few || halves ? pair : (width == 128 ? 0.34 : 0.535) * 1.65;
     const double saved = tail ? (tail == 128 ? 0.435 : 0.21) / (double)row_tiles : 0.0;  // by narrow last workgroups
     for (int s = 1; s <= kMostSplits && (s == 1 || (tiles / s >= 4 && pairs * row_tiles * s <= kMostShared)); ++s) {
       const int64_t groups = pairs * row_tiles * s, last = groups % at_once;
       if (halves && (tiles / s < 8 || (!ragged && groups > at_once))) continue;
       const double here = (double)((tiles + s - 1) / s);
-      double us, join = s > 1 ? 6.0 + (double)pairs * (double)rows * s * 66 * 8 / 4.4e6 * (ragged ? 0.4 : 1.0) : 0.0;
+      double us, join = s > 1 ? (few ? 4.0 : 6.0) + (double)pairs * (double)rows * s * 66 * 8 / 4.4e6 * (ragged ? 0.4 : 1.0) : 0.0;
       if (ragged) {
-        const double ends = width == 128 ? 5.0 : 8.0;
+        const double ends = few ? 3.8 : width == 128 ? 5.0 : 8.0;
         us = 0.4 * (double)groups / (double)at_once * (pair * here + ends) + alone * here + ends + join;
+      } else if (few) {
+        us = (double)((groups + at_once - 1) / at_once) * (3.8 + pair * here) + join;
       } else {
         const double rounds = (double)(groups / at_once) * pair + (last == 0 ? 0.0 : last <= 256 ? alone : pair);
         us = rounds * (groups > at_once ? 1.0 - saved : 1.0) * here + 4.0 + halves + join;
       }
       if (best < 0 || us < best) {
         best = us;
-        p.width = width;
+        p.wide = !few;
+        p.width = few ? 0 : width;
         p.tail = tail;
         p.halves = halves;
         p.row_tiles = row_tiles;

@@ -204,9 +204,9 @@ DRIVER = r"""
 #include "agg_cross_plan.h"
 int main() {
   long long pairs, rows, keys;
-  int ragged, fits;
-  while (scanf("%lld %lld %lld %d %d", &pairs, &rows, &keys, &ragged, &fits) == 5) {
-    const agg::CrossPlan p = agg::plan_cross(pairs, rows, keys, ragged, fits);
+  int ragged, fits, paged;
+  while (scanf("%lld %lld %lld %d %d %d", &pairs, &rows, &keys, &ragged, &fits, &paged) == 6) {
+    const agg::CrossPlan p = agg::plan_cross(pairs, rows, keys, ragged, fits, paged);
     printf("%d %d %d %lld %d\n", p.wide ? p.width : 16 * p.tiles, p.tail, p.halves, (long long)p.row_tiles, p.splits);
   }
 }
@@ -221,7 +221,7 @@ def plan(tmp_path_factory):
                            "-o", str(d / "plan"), str(d / "plan.cpp")])
 
     def ask(sizes):
-        text = "".join("%d %d %d %d %d\n" % s for s in sizes)
+        text = "".join("%d %d %d %d %d %d\n" % s for s in sizes)
         out = subprocess.run([str(d / "plan")], input=text, text=True, check=True, stdout=subprocess.PIPE).stdout
         return [tuple(int(x) for x in line.split()) for line in out.splitlines()]
 
@@ -229,13 +229,13 @@ def plan(tmp_path_factory):
 
 
 def test_every_row_has_a_workgroup_and_every_split_keys(plan):
-    sizes = [(pairs, rows, keys, ragged, fits) for pairs in (1, 3, 16, 100, 4096, 2 ** 31 - 1)
+    sizes = [(pairs, rows, keys, ragged, fits, paged) for pairs in (1, 3, 16, 100, 4096, 2 ** 31 - 1)
              for rows in (1, 16, 17, 33, 64, 65, 257, 400, 1374, 10992, 2 ** 30)
-             for keys in (0, 1, 31, 64, 1000, 20000, 137400, 2 ** 31 - 600) for ragged in (0, 1) for fits in (0, 1)]
-    for (pairs, rows, keys, ragged, fits), (width, tail, halves, row_tiles, splits) in zip(sizes, plan(sizes)):
+             for keys in (0, 1, 31, 64, 1000, 20000, 137400, 2 ** 31 - 600) for ragged in (0, 1) for fits in (0, 1) for paged in (0, 1)]
+    for (pairs, rows, keys, ragged, fits, _), (width, tail, halves, row_tiles, splits) in zip(sizes, plan(sizes)):
         assert row_tiles * width >= rows > (row_tiles - 1) * width
         assert width in (16, 32, 128, 256) and (fits or width < 128)
-        assert (width >= 128) == (fits and (rows > 64 or rows > 32 and pairs * 2 > 256))
+        assert width < 128 or rows > 32
         assert tail in (0, 128, 192) and (tail == 0 or (width == 256 and 0 < rows % 256 <= tail))
         assert not halves or (width == 128 and (ragged or pairs * row_tiles * splits <= 256))
         assert 1 <= splits <= 64 and (splits == 1 or keys // splits >= (192 if width >= 128 else 1))
@@ -243,23 +243,28 @@ def test_every_row_has_a_workgroup_and_every_split_keys(plan):
 
 def test_parts_of_a_batch_share_out_no_keys(plan):
     """More workgroups than a launch takes: no splits, whose partial results a launch of its own could not find."""
-    sizes = [(pairs, rows, 2 ** 31 - 600, ragged, 1) for pairs in (2 ** 22, 2 ** 23 + 5, 2 ** 31 - 1) for rows in (65, 256, 1000)
-             for ragged in (0, 1)]
+    sizes = [(pairs, rows, 2 ** 31 - 600, ragged, 1, paged) for pairs in (2 ** 22, 2 ** 23 + 5, 2 ** 31 - 1) for rows in (65, 256, 1000)
+             for ragged in (0, 1) for paged in (0, 1)]
     assert all(p[-1] == 1 for p in plan(sizes))
 
 
 def test_sizes_reach_their_kernels(plan):
-    """The GPU tests' sizes run every kernel, with and without shared out keys."""
+    """The GPU tests' sizes run every kernel, out of pages and in place, with and without shared out keys."""
     import test_gpu_cross as gpu
 
-    asked = [(B * 2, NQ, NK, 0, 1) for B, NQ, NK in gpu.LENGTHS] + [(B * Hk, NQ * (H // Hk), NK, 0, 1) for B, NQ, NK, H, Hk in gpu.WIDE]
-    reached = {(width, tail, halves, splits > 1) for width, tail, halves, _, splits in plan(asked)}
-    for kernel in [(16, 0, 0), (32, 0, 0), (128, 0, 0), (256, 0, 0), (256, 128, 0)]:
-        assert kernel + (False,) in reached and kernel + (True,) in reached, kernel
-    assert (256, 192, 0, False) in reached and (128, 0, 1, False) in reached and (128, 0, 1, True) in reached
-    redone = {(width, tail, halves, splits > 1)
-              for width, tail, halves, _, splits in plan([(B * H, NQ, NK, 0, 1) for B, NQ, NK, H in gpu.REDO])}
-    assert {k for k in reached if k[0] >= 128} == redone
+    for paged in (0, 1):
+        def reached(sizes):
+            asked = [(B * Hk, NQ * (H // Hk), NK, 0, 1, paged) for B, NQ, NK, H, Hk in sizes]
+            return {(width, tail, halves, splits > 1) for width, tail, halves, _, splits in plan(asked)}
+
+        got = reached([(B, NQ, NK, 2, 2) for B, NQ, NK in gpu.LENGTHS] + gpu.WIDE)
+        for kernel in [(16, 0, 0), (32, 0, 0), (128, 0, 0), (128, 0, 1), (256, 0, 0), (256, 128, 0)]:
+            assert kernel + (False,) in got and kernel + (True,) in got, (paged, kernel)
+        assert (256, 192, 0, False) in got
+        wide = {k[:3] for k in got if k[0] >= 128}
+        behind = [(len(lens) * H, NQ, NK, len(lens) > 1, 1, paged) for NQ, H, NK, lens in gpu.BEHIND]
+        assert {k[:3] for k in plan(behind) if k[0] >= 128} >= wide - {(256, 192, 0)}, paged
+        assert {k for k in got if k[0] >= 128} == {k for k in reached([(B, NQ, NK, H, H) for B, NQ, NK, H in gpu.REDO]) if k[0] >= 128}, paged
 
 
 # ---- the code that is built ----------------------------------------------------------------------------

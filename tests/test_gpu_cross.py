@@ -116,10 +116,11 @@ def test_lengths(B, NQ, NK):
     both(B, NQ, NK, 2)
 
 
-# sizes that fill the card with workgroups of 256 rows: B, NQ, NK, H, H_kv
+# sizes that fill the card with workgroups of every width: B, NQ, NK, H, H_kv
 WIDE = [(20, 512, 90, 16, 16), (24, 512, 400, 16, 16), (20, 520, 130, 16, 16), (20, 440, 100, 16, 16), (16, 190, 65, 32, 16), (1, 1374, 9000, 16, 16),
         (2, 700, 6000, 16, 8), (1, 2816, 8000, 16, 16), (6, 128, 700, 4, 4), (3, 500, 1500, 16, 4), (2, 1024, 12000, 16, 16),
-        (1, 600, 20000, 2, 2), (3, 380, 9000, 1, 1)]
+        (1, 600, 20000, 2, 2), (3, 380, 9000, 1, 1), (20, 100, 100, 4, 4), (20, 100, 2000, 4, 4), (2, 440, 5000, 12, 12),
+        (24, 65, 1029, 4, 4), (6, 65, 2000, 16, 16)]
 
 
 @pytest.mark.parametrize("B, NQ, NK, H, H_kv", WIDE)
@@ -139,13 +140,14 @@ def test_heads(H, H_kv, NQ):
     both(2, NQ, 197, H, H_kv, seed=2)
 
 
-@pytest.mark.parametrize("NQ, NK", [(1, 700), (9, 5000), (40, 300), (100, 640), (300, 1400), (520, 9000)])
-def test_ragged(NQ, NK):
+@pytest.mark.parametrize("NQ, NK, H", [(1, 700, 3), (9, 5000, 3), (40, 300, 3), (100, 640, 3), (300, 1400, 3), (520, 9000, 3),
+                                       (100, 640, 24), (300, 1400, 16), (700, 500, 16)])
+def test_ragged(NQ, NK, H):
     """Lengths of every kind: none, one, inside a tile, on its border, all, and values outside the range."""
     k_lens = [NK, 0, 1, NK // 2, 64, min(65, NK), NK - 1, -3, NK + 100]
     q_lens = [NQ, NQ, 1, NQ // 2, 0, NQ - 1, NQ, NQ, NQ + 7]
-    both(9, NQ, NK, 3, seed=3, k_lens=k_lens)
-    both(9, NQ, NK, 2, 1, seed=4, q_lens=q_lens, k_lens=k_lens)
+    both(9, NQ, NK, H, seed=3, k_lens=k_lens)
+    both(9, NQ, NK, H - H % 2, H // 2, seed=4, q_lens=q_lens, k_lens=k_lens)
     both(3, NQ, NK, 2, seed=5, q_lens=[0, 0, 0], k_lens=[0, 5, NK])
 
 
@@ -164,17 +166,20 @@ def test_no_queries_and_no_keys():
     assert not bool(o.any()) and bool((lse == -math.inf).all())
 
 
-@pytest.mark.parametrize("NQ", [1, 20, 60, 130, 400])
-def test_what_lies_behind_the_keys_does_not_matter(NQ):
+BEHIND = [(NQ, H, 1000, (1000, 1, 95, 640)) for NQ, H in [(1, 2), (20, 2), (60, 2), (250, 32), (500, 32), (1000, 16)]] + \
+         [(1374, 16, 9000, (8963,)), (2816, 16, 8000, (7990,)), (100, 80, 100, (70,)), (512, 350, 400, (391,)), (65, 96, 1029, (1001,))]
+
+
+@pytest.mark.parametrize("NQ, H, NK, lens", BEHIND)
+def test_what_lies_behind_the_keys_does_not_matter(NQ, H, NK, lens):
     """NaN and infinities in rows, and in pages, behind the last key."""
     g = gen(7)
-    B, NK, H = 4, 1000, 2
-    lens = [1000, 1, 95, 640]
+    B, lens = len(lens), list(lens)
     q, k, v = bf16(g, B, NQ, H, 64), bf16(g, B, NK, H, 64), bf16(g, B, NK, H, 64)
     kl = ints(lens)
     cross = agg.make_cross(B, NQ, NK, H, k_lens=kl)
     want = harness.cross_forward(cross, q, k, v)
-    pages, n = pages_of(g, B, 16)
+    pages, n = pages_of(g, B, -(-NK // 64))
     pools = harness.make_pools(n, H, "cuda", fill=0)
     put(pools, pages, k, v, lens)
     clean = harness.cache_forward(agg.make_cache(*pools, pages, H), cross, q)
@@ -224,8 +229,8 @@ def test_large_logits(NQ, NK):
 
 
 # a size for each wide kernel, with and without shared out keys: B, NQ, NK, H
-REDO = [(20, 440, 100, 16), (24, 512, 400, 16), (20, 520, 130, 16), (1, 1374, 9000, 16), (1, 2816, 8000, 16), (1, 777, 1029, 2),
-        (1, 600, 20000, 2), (1, 90, 5000, 2), (2, 130, 200, 2)]
+REDO = [(20, 440, 100, 16), (24, 512, 400, 16), (20, 520, 130, 16), (1, 1374, 9000, 16), (1, 2816, 8000, 16), (2, 440, 5000, 12),
+        (20, 100, 100, 4), (20, 100, 2000, 4), (24, 65, 1029, 4), (6, 65, 2000, 16)]
 
 
 @pytest.mark.parametrize("B, NQ, NK, H", REDO)
@@ -248,13 +253,13 @@ def test_rows_redone_on_every_route(B, NQ, NK, H):
         check(cross, harness.cache_forward(agg.make_cache(*pools, pages, H), cross, q2), q2, k2, v, what="cached, key %d" % at)
 
 
-@pytest.mark.parametrize("NQ", [3, 50, 300])
-def test_rows_that_are_no_numbers(NQ):
+@pytest.mark.parametrize("NQ, H", [(3, 2), (50, 2), (300, 2), (300, 16), (600, 32)])
+def test_rows_that_are_no_numbers(NQ, H):
     """A query that is NaN spoils its own row, a key that is NaN its sequence, a value that is NaN its channel."""
-    say("not numbers", NQ)
+    say("not numbers", NQ, H)
     g = gen(9)
-    q, k, v = bf16(g, 2, NQ, 2, 64), bf16(g, 2, 200, 2, 64), bf16(g, 2, 200, 2, 64)
-    cross = agg.make_cross(2, NQ, 200, 2)
+    q, k, v = bf16(g, 2, NQ, H, 64), bf16(g, 2, 200, H, 64), bf16(g, 2, 200, H, 64)
+    cross = agg.make_cross(2, NQ, 200, H)
     want, _ = harness.cross_forward(cross, q, k, v)
     _, _, size, dots = orc.attention(q, k, v, 0.125)
     q2 = q.clone()
@@ -282,12 +287,12 @@ def test_rows_that_are_no_numbers(NQ):
     assert bool((o[0, :, 1, 9] == math.inf).all()) and int(torch.isfinite(o).logical_not().sum()) == NQ
 
 
-@pytest.mark.parametrize("NQ, NK", [(1, 3000), (40, 301), (300, 777)])
-def test_strides(NQ, NK):
+@pytest.mark.parametrize("NQ, NK, H_kv", [(1, 3000, 3), (40, 301, 3), (300, 777, 3), (300, 777, 24), (600, 777, 24)])
+def test_strides(NQ, NK, H_kv):
     """Keys and values side by side, queries among other channels: the results of contiguous ones, to the bit."""
-    say("strides", NQ, NK)
+    say("strides", NQ, NK, H_kv)
     g = gen(10)
-    B, H, H_kv = 2, 6, 3
+    B, H = 2, 2 * H_kv
     q, k, v = bf16(g, B, NQ, H, 64), bf16(g, B, NK, H_kv, 64), bf16(g, B, NK, H_kv, 64)
     lens = ints([NK - 5, NK])
     cross = agg.make_cross(B, NQ, NK, H, H_kv, k_lens=lens)
@@ -310,18 +315,19 @@ def test_strides(NQ, NK):
         assert same_bits(x, y)
 
 
-def test_shared_and_foreign_pages():
+@pytest.mark.parametrize("H", [2, 32])
+def test_shared_and_foreign_pages(H):
     """Sequences over one row of the table with lengths of their own, and page numbers outside the pool, which are read as
     the first or the last page."""
-    say("pages")
+    say("pages", H)
     g = gen(11)
-    H, NK = 2, 500
+    NK = 500
     k, v = bf16(g, 1, NK, H, 64), bf16(g, 1, NK, H, 64)
     pages, n = pages_of(g, 1, 8)
     pools = harness.make_pools(n, H, "cuda", fill=0)
     put(pools, pages, k, v)
     lens = [100, 250, 500, 0, 33]
-    for NQ in (2, 150):
+    for NQ in (2, 150, 600):
         q = bf16(g, 5, NQ, H, 64)
         shared = pages.expand(5, 8).contiguous()
         kl = ints(lens)
@@ -619,9 +625,9 @@ def test_streams_and_graphs():
 def test_results_repeat_to_the_bit():
     say("repeat")
     g = gen(33)
-    for B, NQ, NK in ((1, 1, 30000), (2, 50, 4000), (1, 700, 5000)):
-        q, k, v = bf16(g, B, NQ, 3, 64), bf16(g, B, NK, 3, 64), bf16(g, B, NK, 3, 64)
-        cross = agg.make_cross(B, NQ, NK, 3)
+    for B, NQ, NK, H in ((1, 1, 30000, 3), (2, 50, 4000, 3), (1, 700, 5000, 3), (1, 1374, 9000, 16), (6, 65, 2000, 16)):
+        q, k, v = bf16(g, B, NQ, H, 64), bf16(g, B, NK, H, 64), bf16(g, B, NK, H, 64)
+        cross = agg.make_cross(B, NQ, NK, H)
         first = harness.cross_forward(cross, q, k, v)
         for _ in range(3):
             again = harness.cross_forward(cross, q, k, v)
@@ -630,7 +636,7 @@ def test_results_repeat_to_the_bit():
 
 
 # ---- sizes beyond 32 bits ------------------------------------------------------------------------
-@pytest.mark.parametrize("NQ", [3, 200])
+@pytest.mark.parametrize("NQ", [3, 200, 1500])
 def test_offsets_beyond_32_bits(NQ):
     """A pool of 9 GiB whose used pages lie at its end, and rows 2 MiB apart."""
     say("far offsets", NQ)
