@@ -65,24 +65,35 @@ inline CrossPlan plan_cross(int64_t pairs, int64_t rows, int64_t keys, bool ragg
   p.splits = 0;
   for (int kind = 0; kind < 4; ++kind) {
     const int width = kind == 0 ? kWideRows : kind == 3 ? kFewRows : 128, halves = kind == 2, few = kind == 3;
-    const int64_t row_tiles = (rows + width - 1) / width, at_once = halves || few ? 256 : 512;
+    const int64_t row_tiles = (rows + width - 1) / width;
+    const int log_at_once = halves || few ? 8 : 9;
+    const int64_t at_once = (int64_t)1 << log_at_once;
     const int rest = (int)(rows % width);
     const int tail = width != kWideRows || rest == 0 ? 0 : rest <= 128 ? 128 : rest <= 192 ? 192 : 0;
     const double pair = few ? (paged ? 0.22 : 0.33) : (halves ? 0.285 : width == 128 ? 0.565 : 1.0) * 1.65;
     const double alone = few || halves ? pair : (width == 128 ? 0.34 : 0.535) * 1.65;
     const double saved = tail ? (tail == 128 ? 0.435 : 0.21) / (double)row_tiles : 0.0;  // by narrow last workgroups
-    for (int s = 1; s <= kMostSplits && (s == 1 || (tiles / s >= 4 && pairs * row_tiles * s <= kMostShared)); ++s) {
-      const int64_t groups = pairs * row_tiles * s, last = groups % at_once;
-      if (halves && (tiles / s < 8 || (!ragged && groups > at_once))) continue;
+    // (few divisions: a call plans up to four times, once for each place that keys may lie in)
+    const int64_t unsplit = pairs * row_tiles;
+    int64_t most = tiles / (halves ? 8 : 4);
+    if (most > kMostSplits) most = kMostSplits;
+    const int64_t room = (halves && !ragged ? at_once : kMostShared) / unsplit;
+    if (most > room) most = room;
+    if (most < 1) {
+      if (halves && (tiles < 8 || (!ragged && room < 1))) continue;
+      most = 1;
+    }
+    for (int s = 1; s <= (int)most; ++s) {
+      const int64_t groups = unsplit * s, last = groups & (at_once - 1);
       const double here = (double)((tiles + s - 1) / s);
       double us, join = s > 1 ? (few ? 4.0 : 6.0) + (double)pairs * (double)rows * s * 66 * 8 / 4.4e6 * (ragged ? 0.4 : 1.0) : 0.0;
       if (ragged) {
         const double ends = few ? 3.8 : width == 128 ? 5.0 : 8.0;
         us = 0.4 * (double)groups / (double)at_once * (pair * here + ends) + alone * here + ends + join;
       } else if (few) {
-        us = (double)((groups + at_once - 1) / at_once) * (3.8 + pair * here) + join;
+        us = (double)((groups + at_once - 1) >> log_at_once) * (3.8 + pair * here) + join;
       } else {
-        const double rounds = (double)(groups / at_once) * pair + (last == 0 ? 0.0 : last <= 256 ? alone : pair);
+        const double rounds = (double)(groups >> log_at_once) * pair + (last == 0 ? 0.0 : last <= 256 ? alone : pair);
         us = rounds * (groups > at_once ? 1.0 - saved : 1.0) * here + 4.0 + halves + join;
       }
       if (best < 0 || us < best) {
