@@ -52,12 +52,13 @@ __device__ __forceinline__ void store_row(const CrossArgs& a, int b, int hk, uin
 }  // namespace
 
 // ---------------------------------------------------------------------------
-// Few rows a pair: bound by the keys and values, which are read once.  Every wavefront takes 32-key blocks of its own, straight into
-// registers (a page's fragment order is the order of the matrix instruction's operands; rows read in place need one turn of the
-// values through LDS), a block ahead of the one it works on, with the running maximum and sum of an online softmax; the wavefronts
-// of a workgroup, and the workgroups that share a pair's keys, are joined at the end by their references.
+// Few rows a pair, and calls of more that fit on the card at once: bound by the keys and values, which are read once for every 16
+// or 32 rows.  Every wavefront takes 32-key blocks of its own, straight into registers (a page's fragment order is the order of the
+// matrix instruction's operands; rows read in place need one turn of the values through LDS), a block ahead of the one it works on,
+// with the running maximum and sum of an online softmax; the wavefronts of a workgroup, and the workgroups that share a pair's keys,
+// are joined at the end by their references.
 // Measured (16 heads): one query over 137400 keys in pages 97 us = 5.8 TB/s, in place 112 = 5.0 (a device copy: 4.9); 32 rows the
-// same within 5 %; over 262 keys 4.1, nearly all of it latencies one after another.  Four wavefronts of 64 rows: 15.8 us where two
+// same within 5 %; over 262 keys 4.1 to 4.4, nearly all of it latencies one after another.  Four wavefronts of 64 rows: 15.8 us where two
 // workgroups of 32 rows take 9.0 (64 rows, 1374 keys).
 // ---------------------------------------------------------------------------
 constexpr int kFewThreads = 64 * kFewWaves;
