@@ -826,7 +826,7 @@ int agg_mx4_linear_fwd(int64_t rows, int32_t N, int32_t K, const agg_mx4_linear*
 
 size_t agg_cross_workspace_bytes(const agg_cross* cross) {
   if (check_cross(cross) != AGG_OK) return 0;
-  const bool ragged = cross_ragged(cross->B, cross->q_lens, cross->k_lens);
+  const int ragged = cross_ragged(cross->B, cross->q_lens, cross->k_lens);
   return cross_partial_floats(cross->B, cross->NQ, cross->NK, cross->H, cross->H_kv, ragged) * sizeof(float);
 }
 

@@ -650,7 +650,7 @@ static void launch_join(const CrossArgs& a, int splits, int64_t pairs, int64_t r
 // the wide kernel reaches a tile's 64 rows with 32-bit byte offsets
 static bool wide_fits(int64_t stride) { return stride <= ((int64_t)1 << 23); }
 
-size_t cross_partial_floats(int64_t B, int64_t NQ, int64_t NK, int64_t H, int64_t H_kv, bool ragged) {
+size_t cross_partial_floats(int64_t B, int64_t NQ, int64_t NK, int64_t H, int64_t H_kv, int ragged) {
   const int64_t pairs = B * H_kv, rows = NQ * (H / H_kv);
   // where a call's keys lie chooses between three plans: enough for any
   int splits = plan_cross(pairs, rows, NK, ragged, true, true).splits;

@@ -24,9 +24,9 @@ constexpr int kWideRows = 256;  // rows of a wide workgroup
 constexpr int kMostSplits = 64;
 constexpr int kMostShared = 4096;  // most workgroups of a call that is shared out along the keys
 
-// wide_fits: the distances between rows are what the wide kernel can address; ragged: the sequences may have different lengths;
-// paged: keys and values in a cache
-inline CrossPlan plan_cross(int64_t pairs, int64_t rows, int64_t keys, bool ragged, bool wide_fits, bool paged) {
+// wide_fits: the distances between rows are what the wide kernel can address; ragged: the sequences may have different lengths, 2: of
+// queries and of keys; paged: keys and values in a cache
+inline CrossPlan plan_cross(int64_t pairs, int64_t rows, int64_t keys, int ragged, bool wide_fits, bool paged) {
   CrossPlan p;
   p.wide = p.width = p.tail = p.halves = 0;
   p.tiles = rows <= 16 ? 1 : 2;
@@ -58,8 +58,18 @@ inline CrossPlan plan_cross(int64_t pairs, int64_t rows, int64_t keys, bool ragg
   // 512 to 512 6.3 / 8.9, 64 to 137400 106 / 105, 64 of 24 sequences to 1374 45.7 / 26.1; in place 261 to 1374 11.9 / 13.3, 522 to 522
   // 13.8 / 9.6.)
   // Like sequences: rounds of as many workgroups as run at once, eight wavefronts where that is one round.  Sequences of different
-  // lengths: 0.4 of the work is taken to be there, and a longest piece behind it (fitted to eight such calls, of which
-  // it takes what is 0 to 10 % off the fastest).
+  // lengths, which the host does not know: their throughput, and a longest piece behind it, by constants fitted to 693 calls of 33 to 8000
+  // rows a pair with random lengths, every kernel with up to 64 splits.  (Their choice is 4 % behind the fastest in the mean and 14 % at the
+  // ninth decile; 0.4 of the full work at the rates above 8 % and 29 %: 36 queries of 8 sequences to 13740 cached keys, 16 heads, 64.1 us
+  // against 48.0, 56 to 2878, 20 / 4 heads, 26.6 against 19.5.)  Where queries end early too there is less work: 0.8 of the first
+  // term (349 such calls: 4 % behind with 0.8 as with 1, 8 % with 0.5).
+  struct Ragged {
+    double tile, ends;            // of a workgroup among as many as run at once
+    double last_tile, last_ends;  // of the last ones
+    double join, bytes;           // of the second launch
+  };
+  static constexpr Ragged kRagged[] = {{0.53, 5.3, 1.65, 14.2, 6.0, 0.67}, {0.37, 6.4, 0.84, 5.6, 6.0, 0.67}, {0.25, 7.1, 0.48, 6.2, 6.0, 0.67},
+                                       {0.31, 6.1, 0.37, 1.0, 1.25, 1.29}, {0.34, 5.7, 0.21, 1.5, 1.25, 1.29}};  // kinds 0 to 3; 3 out of pages
   const int64_t tiles = (keys + 63) / 64;
   double best = -1;
   p.splits = 0;
@@ -86,10 +96,13 @@ inline CrossPlan plan_cross(int64_t pairs, int64_t rows, int64_t keys, bool ragg
     for (int s = 1; s <= (int)most; ++s) {
       const int64_t groups = unsplit * s, last = groups & (at_once - 1);
       const double here = (double)((tiles + s - 1) / s);
-      double us, join = s > 1 ? (few ? 4.0 : 6.0) + (double)pairs * (double)rows * s * 66 * 8 / 4.4e6 * (ragged ? 0.4 : 1.0) : 0.0;
+      const double bytes = (double)pairs * (double)rows * s * 66 * 8 / 4.4e6;  // us of the partial results' way
+      const double join = s > 1 ? (few ? 4.0 : 6.0) + bytes : 0.0;
+      double us;
       if (ragged) {
-        const double ends = few ? 3.8 : width == 128 ? 5.0 : 8.0;
-        us = 0.4 * (double)groups / (double)at_once * (pair * here + ends) + alone * here + ends + join;
+        const Ragged& r = kRagged[few && paged ? 4 : kind];
+        us = (ragged == 2 ? 0.8 : 1.0) * (double)groups / (double)at_once * (r.tile * here + r.ends) + r.last_tile * here +
+             r.last_ends + (s > 1 ? r.join + r.bytes * bytes : 0.0);
       } else if (few) {
         us = (double)((groups + at_once - 1) >> log_at_once) * (3.8 + pair * here) + join;
       } else {

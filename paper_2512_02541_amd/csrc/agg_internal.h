@@ -240,10 +240,10 @@ struct CrossArgs {
   float* lse;
   float* partial;  // workspace
 };
-// whether the sequences of a call may have different lengths
-inline bool cross_ragged(int32_t B, const int32_t* q_lens, const int32_t* k_lens) { return B > 1 && (q_lens || k_lens); }
+// whether the sequences of a call may have different lengths: 0: no, 2: of queries and of keys, 1: of one of them
+inline int cross_ragged(int32_t B, const int32_t* q_lens, const int32_t* k_lens) { return B > 1 ? (q_lens != nullptr) + (k_lens != nullptr) : 0; }
 // floats of workspace
-size_t cross_partial_floats(int64_t B, int64_t NQ, int64_t NK, int64_t H, int64_t H_kv, bool ragged);
+size_t cross_partial_floats(int64_t B, int64_t NQ, int64_t NK, int64_t H, int64_t H_kv, int ragged);
 hipError_t launch_cross(const CrossArgs& args, hipStream_t st);
 
 // New tokens of a cache (agg_cache_append).
