@@ -34,10 +34,11 @@ inline CrossPlan plan_cross(int64_t pairs, int64_t rows, int64_t keys, int ragge
   if (rows <= kFewRows || !wide_fits) {
     // Splits by predicted time: a wavefront's steps one after another, and a second launch.  More workgroups than run at once
     // (two on a CU of up to 16 rows, one of more) gain nothing where the sequences are alike: the memory is busy with them.  Where they
-    // are not, the long ones would end alone: there more rounds are taken, of 2 us each (us, one token each over up to 10000 keys of 24
-    // sequences, 16 heads: 124 unsplit, 103 / 95 / 91 / 106 with 2 / 4 / 16 / 32 splits).
+    // are not, the long ones would end alone: there more rounds are taken, of 2 us each (us, one token each over up to 10000
+    // keys of 24 sequences, 16 heads: 124 unsplit, 103 / 95 / 91 / 106 with 2 / 4 / 16 / 32 splits; over 250 calls with random lengths
+    // the choice is 4 % behind the fastest in the mean).
     const int64_t groups = pairs * p.row_tiles, steps = (keys + kKeyBlock * kFewWaves - 1) / (kKeyBlock * kFewWaves);
-    const int64_t at_once = p.tiles == 1 ? 512 : 256, most = !ragged ? at_once : p.tiles == 1 ? 4096 : 512;
+    const int64_t at_once = p.tiles == 1 ? 512 : 256, most = !ragged ? at_once : p.tiles == 1 ? 4096 : 1024;
     const double step = p.tiles == 1 ? 0.55 : 0.85;
     double best = 0;
     p.splits = 1;
