@@ -22,7 +22,8 @@ constexpr int kKeyBlock = 32;   // keys of a wavefront's step
 constexpr int kFewRows = 32;    // most rows of such a workgroup
 constexpr int kWideRows = 256;  // rows of a wide workgroup
 constexpr int kMostSplits = 64;
-constexpr int kMostShared = 4096;  // most workgroups of a call that is shared out along the keys
+constexpr int kMostShared = 4096;       // most workgroups of a call that is shared out along the keys
+constexpr int64_t kUncached = 1 << 20;  // keys of all pairs, 256 bytes each with their values, that fill the cache behind the L2s
 
 // wide_fits: the distances between rows are what the wide kernel can address; ragged: the sequences may have different lengths, 2: of
 // queries and of keys; paged: keys and values in a cache
@@ -76,16 +77,17 @@ inline CrossPlan plan_cross(int64_t pairs, int64_t rows, int64_t keys, int ragge
   p.splits = 0;
   for (int kind = 0; kind < 4; ++kind) {
     const int width = kind == 0 ? kWideRows : kind == 3 ? kFewRows : 128, halves = kind == 2, few = kind == 3;
-    const int64_t row_tiles = (rows + width - 1) / width;
+    const int64_t row_tiles = (rows + width - 1) / width, unsplit = pairs * row_tiles;
     const int log_at_once = halves || few ? 8 : 9;
     const int64_t at_once = (int64_t)1 << log_at_once;
     const int rest = (int)(rows % width);
     const int tail = width != kWideRows || rest == 0 ? 0 : rest <= 128 ? 128 : rest <= 192 ? 192 : 0;
     const double pair = few ? (paged ? 0.22 : 0.33) : (halves ? 0.285 : width == 128 ? 0.565 : 1.0) * 1.65;
     const double alone = few || halves ? pair : (width == 128 ? 0.34 : 0.535) * 1.65;
+    // keys that no cache holds come from memory for each 32 rows again (us, 48 rows of 48 pairs to 32099 keys: 135, 128 rows wide 81)
+    const double reads = few && pairs * keys >= kUncached ? (double)unsplit * (double)keys * 256 / 5.2e6 : 0.0;
     const double saved = tail ? (tail == 128 ? 0.435 : 0.21) / (double)row_tiles : 0.0;  // by narrow last workgroups
     // (few divisions: a call plans up to four times, once for each place that keys may lie in)
-    const int64_t unsplit = pairs * row_tiles;
     int64_t most = tiles / (halves ? 8 : 4);
     if (most > kMostSplits) most = kMostSplits;
     const int64_t room = (halves && !ragged ? at_once : kMostShared) / unsplit;
@@ -105,7 +107,9 @@ inline CrossPlan plan_cross(int64_t pairs, int64_t rows, int64_t keys, int ragge
         us = (ragged == 2 ? 0.8 : 1.0) * (double)groups / (double)at_once * (r.tile * here + r.ends) + r.last_tile * here +
              r.last_ends + (s > 1 ? r.join + r.bytes * bytes : 0.0);
       } else if (few) {
-        us = (double)((groups + at_once - 1) >> log_at_once) * (3.8 + pair * here) + join;
+        us = (double)((groups + at_once - 1) >> log_at_once) * (3.8 + pair * here);
+        if (us < reads) us = reads;
+        us += join;
       } else {
         const double rounds = (double)(groups >> log_at_once) * pair + (last == 0 ? 0.0 : last <= 256 ? alone : pair);
         us = rounds * (groups > at_once ? 1.0 - saved : 1.0) * here + 4.0 + halves + join;
