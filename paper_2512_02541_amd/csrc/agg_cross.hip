@@ -274,7 +274,7 @@ __global__ __launch_bounds__(kFewThreads, kJ == 1 ? 4 : 2) void cross_few_kernel
 // shared out along the keys too, each workgroup leaving its sums without (fast path) or with (general path) a reference in the
 // workspace.  A workgroup whose sums leave the fast path's range redoes its rows in place, 128 at a time.
 // Measured: 8 frames over 40 (10992 queries, 54960 keys, 16 heads) 2.04 to 2.17 ms = 1.14 to 1.21 PFLOP/s, of which the joining of four
-// splits is 0.037; the matrix core is busy in 0.63 of the cycles, at 1.93 GHz.  A frame over 137400 cached keys 0.74 to 0.77 ms, 512
+// splits is 0.037; the matrix core is busy in 0.63 of the cycles, at 1.93 GHz.  A frame over 137400 cached keys 0.73 to 0.77 ms, 512
 // queries to each of 24 frames 67 to 78 us.
 // ---------------------------------------------------------------------------
 namespace {

@@ -141,7 +141,8 @@ def test_heads(H, H_kv, NQ):
 
 
 @pytest.mark.parametrize("NQ, NK, H", [(1, 700, 3), (9, 5000, 3), (40, 300, 3), (100, 640, 3), (300, 1400, 3), (520, 9000, 3),
-                                       (100, 640, 24), (300, 1400, 16), (700, 500, 16)])
+                                       (100, 640, 24), (300, 1400, 16), (700, 500, 16),
+                                       (700, 65, 32), (512, 700, 2), (70, 3000, 8), (70, 3000, 2)])
 def test_ragged(NQ, NK, H):
     """Lengths of every kind: none, one, inside a tile, on its border, all, and values outside the range."""
     k_lens = [NK, 0, 1, NK // 2, 64, min(65, NK), NK - 1, -3, NK + 100]
