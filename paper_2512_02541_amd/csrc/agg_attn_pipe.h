@@ -116,12 +116,12 @@ __device__ __forceinline__ void mask_unit(f32x4 (&S)[2 * kJ], int kb, int valid,
 // tile of the output.
 template <int kQB, int kJ>
 struct Wave {
-  Frag Qf[kQB][2 * kJ];    // [qb][2 j + h]: B operand of S^T = K Q^T, pre-multiplied by scale*log2(e)
+  Frag Qf[kQB][2 * kJ];    // [qb][2 j + h]: B operand of S^T = K Q^T, pre-multiplied by scale*log2(e) (exact_logits: as it is)
   f32x4 O[kQB][kJ][4];     // [qb][j][dt]: O^T accumulator; channel = 16 dt + 4 G + r, query = c
   f32x4 S[kQB][2 * kJ];    // [qb][kJ kt + j]: score tiles in flight; key = row_key(4 G + r) + 8 kt
   f32x4 L[kQB][kJ];        // [qb][j]: fast path: element 0 of the lanes G = 0 is the row sum, kept by the matrix core
   float la[kQB][kJ];       // [qb][j]: general path: this lane's part of the row sum
-  float mref[kQB][kJ];     // general path: the row's reference (base-2 logit; exact_logits: plain product)
+  float mref[kQB][kJ];     // general path: the row's reference (base-2 logit; exact_logits: -infinity where it has none yet)
   Frag a[4];               // [2 kt + h]: K fragments of the block whose scores are being computed
   Frag v[4];               // [dt]: V fragments of the block whose P V is being accumulated
   Frag P[kJ];              // [j]: probabilities of the previous unit
@@ -150,17 +150,34 @@ __device__ __forceinline__ void exp_unit(const f32x4 (&S)[2 * kJ], Frag (&P)[kJ]
 // General path: the same, and the sums of each query tile's part (there the vector ALU keeps
 // the sums: the unit's own sum is what tells that a score has run away from the row's reference,
 // and it is needed before the probabilities reach the matrix core)
-template <int kJ, bool kScaled = false>
-__device__ __forceinline__ void exp_unit_sum(const f32x4 (&S)[2 * kJ], Frag (&P)[kJ], float (&l)[kJ], float l2 = 1.f) {
+template <int kJ>
+__device__ __forceinline__ void exp_unit_sum(const f32x4 (&S)[2 * kJ], Frag (&P)[kJ], float (&l)[kJ]) {
 #pragma unroll
   for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int j = 0; j < kJ; ++j) {
-        const float s0 = S[kJ * kt + j][2 * i], s1 = S[kJ * kt + j][2 * i + 1];
-        const float e0 = fast_exp2(kScaled ? s0 * l2 : s0);
-        const float e1 = fast_exp2(kScaled ? s1 * l2 : s1);
+        const float e0 = fast_exp2(S[kJ * kt + j][2 * i]);
+        const float e1 = fast_exp2(S[kJ * kt + j][2 * i + 1]);
+        P[j].u[2 * kt + i] = pack_bf16(e0, e1);
+        l[j] += e0;
+        l[j] += e1;
+      }
+}
+
+// General path of exact_logits: the scores are plain products and become base-2 logits relative to each row's reference in one
+// multiply-add.  The difference is rounded after it is taken: a reference far above or far below these scores costs them no digits.
+template <int kJ>
+__device__ __forceinline__ void exp_unit_relative(const f32x4 (&S)[2 * kJ], Frag (&P)[kJ], float (&l)[kJ], float l2, const float (&ref)[kJ]) {
+#pragma unroll
+  for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < kJ; ++j) {
+        const float e0 = fast_exp2(fmaf(S[kJ * kt + j][2 * i], l2, -ref[j]));
+        const float e1 = fast_exp2(fmaf(S[kJ * kt + j][2 * i + 1], l2, -ref[j]));
         P[j].u[2 * kt + i] = pack_bf16(e0, e1);
         l[j] += e0;
         l[j] += e1;
@@ -467,6 +484,7 @@ constexpr int there_and_back(int i) {
 // Scores of one unit: the 32 keys of block fragments `a` against the 16 kJ queries of block tq.
 // General path: the accumulator starts at minus the row's reference instead of zero, so the
 // scores come out relative to it at no cost (the reference is a float, nothing is split).
+// (Not with exact_logits, whose callers leave it out by kGen = false: it would round the scores to the reference's digits.)
 template <bool kGen, int kQB, int kJ>
 __device__ __forceinline__ void score_unit(const Wave<kQB, kJ>& w, int tq, f32x4 (&Sn)[2 * kJ]) {
   f32x4 init[kJ];
@@ -524,7 +542,7 @@ __device__ __forceinline__ void tile_steps(Wave<kQB, kJ>& w, const u32x4* __rest
     // ---- matrix core, part 1: scores of unit `un` ----
     const bool do_qk = !(kLast && beyond);
     f32x4 Sn[2 * kJ];
-    if (do_qk) score_unit<kGen, kQB, kJ>(w, tq, Sn);
+    if (do_qk) score_unit<kGen && !exact_logits(kSrc), kQB, kJ>(w, tq, Sn);
     if (tq == kQB - 1) {  // that was the block's last unit: fragments of the following block
       if (un / kQB == 0) load_k_frags<kSrc>(lds, cur, 1, fa, w.a);
       else if (!kLast) load_k_frags<kSrc>(lds, nxt, 0, fa, w.a);
@@ -540,10 +558,12 @@ __device__ __forceinline__ void tile_steps(Wave<kQB, kJ>& w, const u32x4* __rest
       if (kLast && valid < kTileRows) mask_unit<kJ>(S, kb, valid, G);
       if (!kGen) {
         exp_unit<kJ, exact_logits(kSrc)>(S, Pn, w.l2);
+      } else if (exact_logits(kSrc)) {
+        exp_unit_relative<kJ>(S, Pn, unit_sum, w.l2, w.mref[qb]);
       } else {
         // the scores are already relative to the row's reference; whether it still holds is
         // looked at below, behind the step's last MFMA
-        exp_unit_sum<kJ, exact_logits(kSrc)>(S, Pn, unit_sum, w.l2);
+        exp_unit_sum<kJ>(S, Pn, unit_sum);
       }
     }
     if (do_qk) {
@@ -594,6 +614,7 @@ __device__ __forceinline__ void tile_steps(Wave<kQB, kJ>& w, const u32x4* __rest
       for (int j = 1; j < kJ; ++j) all += unit_sum[j];
       if (__builtin_amdgcn_ballot_w64(!(all < kUnitHi)) != 0) {
         f32x4 (&S)[2 * kJ] = w.S[qb];
+        float ref[kJ];  // exact_logits: what the unit is taken relative to
 #pragma unroll
         for (int j = 0; j < kJ; ++j) {
           float mx = S[j][0];
@@ -603,13 +624,22 @@ __device__ __forceinline__ void tile_steps(Wave<kQB, kJ>& w, const u32x4* __rest
             for (int r = 0; r < 4; ++r) mx = fmaxf(mx, S[kJ * kt + j][r]);
           mx = quad_max(mx);  // the four lanes of a row agree
           const float old = w.mref[qb][j];
-          if ((exact_logits(kSrc) ? mx * w.l2 : mx) > kLazy) w.mref[qb][j] = old + mx;
-          const float d = w.mref[qb][j] - old;
-          const float f = fast_exp2(exact_logits(kSrc) ? -d * w.l2 : -d);
+          float f;
+          if (exact_logits(kSrc)) {
+            // A row without a reference gets here by itself: relative to -infinity its sum is infinite or no number.  It has none
+            // as long as all its logits are -infinity, whose probabilities are 0 relative to anything.
+            w.mref[qb][j] = fmaxf(old, mx * w.l2);
+            ref[j] = w.mref[qb][j] == -INFINITY ? 0.f : w.mref[qb][j];
+            f = fast_exp2(old - ref[j]);
+          } else {
+            if (mx > kLazy) w.mref[qb][j] = old + mx;
+            const float d = w.mref[qb][j] - old;
+            f = fast_exp2(-d);
 #pragma unroll
-          for (int kt = 0; kt < 2; ++kt)
+            for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) S[kJ * kt + j][r] -= d;
+              for (int r = 0; r < 4; ++r) S[kJ * kt + j][r] -= d;
+          }
 #pragma unroll
           for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
@@ -618,7 +648,8 @@ __device__ __forceinline__ void tile_steps(Wave<kQB, kJ>& w, const u32x4* __rest
         }
 #pragma unroll
         for (int j = 0; j < kJ; ++j) unit_sum[j] = 0.f;
-        exp_unit_sum<kJ, exact_logits(kSrc)>(S, w.P, unit_sum, w.l2);
+        if (exact_logits(kSrc)) exp_unit_relative<kJ>(S, w.P, unit_sum, w.l2, ref);
+        else exp_unit_sum<kJ>(S, w.P, unit_sum);
       }
 #pragma unroll
       for (int j = 0; j < kJ; ++j) w.la[qb][j] += unit_sum[j];
@@ -650,7 +681,7 @@ __device__ __forceinline__ bool key_loop(Wave<kQB, kJ>& w, u32x4* __restrict__ l
 #pragma unroll
   for (int j = 0; j < kJ; ++j) w.P[j].u = u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
-  for (int qb = 0; qb + 1 < kQB; ++qb) score_unit<kGen, kQB, kJ>(w, qb, w.S[qb]);
+  for (int qb = 0; qb + 1 < kQB; ++qb) score_unit<kGen && !exact_logits(kSrc), kQB, kJ>(w, qb, w.S[qb]);
 
   int t = 0, cur = 0;
   bool ok = true;

@@ -350,7 +350,9 @@ __device__ __forceinline__ bool attend_cross(const CrossArgs& p, const CrossPlan
       // the kernels below, in the narrow ones of the fast path too; a build test checks that none does.)
       float zero = 0.f;
       if (kGen) asm volatile("" : "+v"(zero));
-      w.mref[qb][j] = zero;
+      float none = -INFINITY;  // general path: the reference comes with the first unit (agg_attn_pipe.h)
+      if (kGen) asm volatile("" : "+v"(none));
+      w.mref[qb][j] = none;
       w.la[qb][j] = zero;
       w.L[qb][j] = f32x4{zero, zero, zero, zero};
 #pragma unroll
@@ -360,31 +362,9 @@ __device__ __forceinline__ bool attend_cross(const CrossArgs& p, const CrossPlan
         w.O[qb][j][dt] = z;
       }
     }
-  // general path: the reference is the largest of the first 32 keys (agg_attn.hip)
-  auto first_tile = [&]() {
-    if (!kGen) return;
-    const int valid0 = ntiles == 1 ? last_valid : kTileRows;
-#pragma unroll
-    for (int qb = 0; qb < kQB; ++qb) {
-      f32x4 s[2 * kJ];
-      score_unit<kGen, kQB, kJ>(w, qb, s);
-      if (valid0 < 32) mask_unit<kJ>(s, 0, valid0, G);
-#pragma unroll
-      for (int j = 0; j < kJ; ++j) {
-        float mx = s[j][0];
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[kJ * kt + j][r]);
-        mx = quad_max(mx);
-        // a NaN or infinite score cannot serve as reference
-        w.mref[qb][j] = fabsf(mx) < 3.0e38f ? mx : 0.f;
-      }
-    }
-  };
   bool done = true;
   if (!kSplit || ntiles > 0)
-    done = key_loop<kSrc, kGen, kSplit, kQB, kJ>(w, lds, votes, src, ntiles, last_valid, tid, wave, fa, G, first_tile);
+    done = key_loop<kSrc, kGen, kSplit, kQB, kJ>(w, lds, votes, src, ntiles, last_valid, tid, wave, fa, G, [] {});
   if (kSplit) {
     // a loop passes one barrier per tile: the shorter one makes up for its missing tile.  Without a reference the two halves'
     // sums and accumulators just add: the second group's go through its LDS, [register][wavefront][lane], to the first
@@ -444,7 +424,7 @@ __device__ __forceinline__ bool attend_cross(const CrossArgs& p, const CrossPlan
         for (int dt = 0; dt < 4; ++dt) *reinterpret_cast<f32x4*>(p.partial + at * kHeadDim + 16 * dt + 4 * eG) = w.O[qb][j][dt];
         if (eG == 0)
           *reinterpret_cast<f32x2*>(partial_sums(p, pairs, plan.splits) + at * 2) =
-              f32x2{kGen ? w.mref[qb][j] * p.scale2 : 0.f, l_fin[qb][j]};
+              f32x2{kGen ? w.mref[qb][j] : 0.f, l_fin[qb][j]};
       }
     return true;
   }
@@ -461,7 +441,7 @@ __device__ __forceinline__ bool attend_cross(const CrossArgs& p, const CrossPlan
         *reinterpret_cast<u32x2*>(epi + (16 * j + ec) * kEpiStride + 16 * dt + 4 * eG) = pack4(w.O[qb][j][dt] * inv);
       if (p.lse && eG == 0 && r0 + 16 * j + ec < row_end) {
         const RowPlace at = row_place(p, hk, r0 + 16 * j + ec);
-        p.lse[((int64_t)b * p.H + at.head) * p.NQ + at.q] = ((kGen ? w.mref[qb][j] * p.scale2 : 0.f) + log2f(l)) * kLn2;
+        p.lse[((int64_t)b * p.H + at.head) * p.NQ + at.q] = ((kGen ? w.mref[qb][j] : 0.f) + log2f(l)) * kLn2;
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");

@@ -1,0 +1,100 @@
+"""Attention to keys of another length where logits and values lie far apart, on the GPU, against float64.
+
+Tolerances count roundings of the keys that carry weight, and of no others.  With p a key's probability, S the sum of |scale q k| over its
+channels (S* that of the row's largest logit) and v its value:
+  a logit is a sum of 64 exact products in float32: 64 * 2^-24 = 2^-18 of S, and so is the largest, which the others are taken relative to:
+      d = 2^-18 (S + S*)
+  O    a probability is rounded to bf16 on its way into the second product, 2^-8, and the sum may hold the rounded or the unrounded
+       ones, 2^-8 more; float32 steps behind it 2^-12: sum of p (2^-7 + 2^-12 + d) |v|, by the sum |O| sum of p d, by the result's rounding 2^-8 |O|
+  lse  sum of p d; 2^-16 (1 + |lse|) for the logarithm and the base; 2^-8 where the sum is that of rounded probabilities
+Keys whose probability is zero in float64 count as nothing, whatever their logit.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2512_02541_amd import binding as agg
+from paper_2512_02541_amd import harness
+
+from test_gpu_cross import bf16, gen, pages_of, put, say
+
+pytestmark = pytest.mark.gpu
+
+HALF = 2.0 ** -8
+DOT = 2.0 ** -18
+
+
+def judge(cross, got, q, k, v, what):
+    """O and lse of calls without lengths.  Where float64 has no number, O has to be none either."""
+    torch.cuda.synchronize()
+    o, lse = got
+    scale, group = float(np.float32(cross.scale)), cross.H // cross.H_kv
+    for b in range(cross.B):
+        for h in range(cross.H):
+            qh, kh, vh = (x.double() for x in (q[b, :, h], k[b, :, h // group], v[b, :, h // group]))
+            logit = (qh @ kh.t().contiguous()) * scale
+            p = torch.softmax(logit, -1)
+            S = (qh.abs() @ kh.abs().t().contiguous()) * scale
+            S = torch.where(p > 0, S, torch.zeros_like(S))
+            d = DOT * (S + S.gather(1, logit.argmax(1, keepdim=True)))
+            want = p @ vh
+            pd = (p * d).sum(1, keepdim=True)
+            tol = (p * (2 * HALF + 2.0 ** -12 + d)) @ vh.abs() + want.abs() * (pd + HALF)
+            off = (o[b, :, h].double() - want).abs()
+            none = torch.isnan(want)
+            assert bool(torch.isnan(o[b, :, h])[none].all()), what + ": numbers where there are none"
+            bad = ~(off <= tol) & ~none
+            assert not bool(bad.any()), "%s, element %d head %d: %d of O off, worst %.3g of the tolerance" % (
+                what, b, h, int(bad.sum()), float((off / tol)[~none].nan_to_num(1e9).max()))
+            wl = torch.logsumexp(logit, -1)
+            loff = (lse[b, h].double() - wl).abs()
+            there = ~none[:, 0]
+            lbad = there & ~(loff <= pd[:, 0] + HALF + 2.0 ** -16 * (1 + wl.abs()))
+            assert not bool(lbad.any()), "%s, element %d head %d: %d of lse off, worst %.3g" % (
+                what, b, h, int(lbad.sum()), float(loff[there].nan_to_num(1e9).max()))
+
+
+def both_places(q, k, v, what):
+    """The call with keys in place and out of a cache."""
+    (B, NQ, H, _), (_, NK, H_kv, _) = q.shape, k.shape
+    cross = agg.make_cross(B, NQ, NK, H, H_kv)
+    say(what, "in place")
+    judge(cross, harness.cross_forward(cross, q, k, v), q, k, v, what)
+    pages, n = pages_of(gen(99), B, -(-NK // 64))
+    pools = harness.make_pools(n, H_kv, "cuda")
+    put(pools, pages, k, v)
+    say(what, "paged")
+    judge(cross, harness.cache_forward(agg.make_cache(*pools, pages, H_kv), cross, q), q, k, v, what + " paged")
+
+
+# B, NQ, NK, H: every wide kernel, keys shared out or not, joined by one and by sixteen groups of lanes, and the kernel of few rows
+KERNELS = [(20, 440, 100, 16), (6, 512, 400, 64), (20, 520, 130, 16), (1, 1374, 9000, 16), (1, 2816, 8000, 16), (2, 440, 5000, 12),
+           (20, 100, 100, 4), (20, 100, 2000, 4), (24, 65, 1029, 4), (6, 65, 2000, 16), (1, 1374, 9000, 1), (2, 700, 9000, 2), (1, 700, 20000, 1),
+           (1, 20, 7001, 2), (1, 1, 20001, 2)]
+
+
+def spikes(q, k, u, at):
+    """Every fiftieth query leaves the fast path's window by the keys `at`: logits of some 280."""
+    q[:, ::50, :, 1:] = (6 * u[1:]).to(torch.bfloat16)
+    k[:, at, :, 1:] = (6 * u[1:]).to(torch.bfloat16)
+
+
+@pytest.mark.parametrize("B, NQ, NK, H", KERNELS)
+def test_keys_hidden_by_value(B, NQ, NK, H):
+    """A channel of the keys hides the first half of every tile of 64, the keys that any share of a sequence begins with: by a little, by much and
+    by -infinity; the others at ordinary logits, and far below zero."""
+    g = gen(41)
+    u = torch.sign(torch.randn(64, generator=g, device="cuda"))
+    q, k, v = bf16(g, B, NQ, H, 64), bf16(g, B, NK, H, 64, scale=0.5), bf16(g, B, NK, H, 64)
+    q[..., 0], k[..., 0] = 1.0, 0.0
+    spikes(q, k, u, [NK - 1])
+    hidden = torch.arange(NK, device="cuda") % 64 < 32
+    hidden[NK - 1] = False
+    for mask in (-8e4, -8e6, -8e9, -math.inf):
+        for below in (0, -160):
+            k2 = k.clone()
+            k2[..., 0] = below * 8.0
+            k2[:, hidden, :, 0] = mask
+            both_places(q, k2, v, "hidden by %g, others at %d" % (mask, below))
