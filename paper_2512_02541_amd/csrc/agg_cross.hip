@@ -271,8 +271,7 @@ __global__ __launch_bounds__(kFewThreads, kJ == 1 ? 4 : 2) void cross_few_kernel
 // ---------------------------------------------------------------------------
 // Many rows a pair: the pipeline of agg_attn.hip over keys that end where the sequence's do, bound like it by the matrix core
 // and the vector ALU together, and by power.  256 rows a workgroup, 128 or 192 in a pair's last one, or 128 in all; few pairs are
-// shared out along the keys too, each workgroup leaving its sums without (fast path) or with (general path) a reference in the
-// workspace.  A workgroup whose sums leave the fast path's range redoes its rows in place, 128 at a time.
+// shared out along the keys too, each workgroup leaving its sums in the workspace, with a reference that makes them 1/2 to 1.  A workgroup whose sums leave the fast path's range redoes its rows in place, 128 at a time.
 // Measured: 8 frames over 40 (10992 queries, 54960 keys, 16 heads) 2.04 to 2.17 ms = 1.14 to 1.21 PFLOP/s, of which the joining of four
 // splits is 0.037; the matrix core is busy in 0.63 of the cycles, at 1.93 GHz.  A frame over 137400 cached keys 0.73 to 0.77 ms, 512
 // queries to each of 24 frames 67 to 78 us.
@@ -420,11 +419,19 @@ __device__ __forceinline__ bool attend_cross(const CrossArgs& p, const CrossPlan
         const uint32_t row = r_wave + (qb * kJ + j) * 16 + ec;
         if (row >= row_end) continue;
         const size_t at = partial_row(p, pairs, split, pair, row);
+        // The join weighs by references, and these are no measure of the sums: 0 (fast path, sums of 2^-90 to 2^90), or the
+        // largest logit of some unit.  The sum's power of two goes over to the reference.  (0 of a sum that is 0 or no number.)
+        const int e = __builtin_amdgcn_frexp_expf(l_fin[qb][j]);
 #pragma unroll
-        for (int dt = 0; dt < 4; ++dt) *reinterpret_cast<f32x4*>(p.partial + at * kHeadDim + 16 * dt + 4 * eG) = w.O[qb][j][dt];
+        for (int dt = 0; dt < 4; ++dt) {
+          f32x4 part;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) part[r] = ldexpf(w.O[qb][j][dt][r], -e);
+          *reinterpret_cast<f32x4*>(p.partial + at * kHeadDim + 16 * dt + 4 * eG) = part;
+        }
         if (eG == 0)
           *reinterpret_cast<f32x2*>(partial_sums(p, pairs, plan.splits) + at * 2) =
-              f32x2{kGen ? w.mref[qb][j] : 0.f, l_fin[qb][j]};
+              f32x2{(kGen ? w.mref[qb][j] : 0.f) + (float)e, ldexpf(l_fin[qb][j], -e)};
       }
     return true;
   }

@@ -98,3 +98,29 @@ def test_keys_hidden_by_value(B, NQ, NK, H):
             k2[..., 0] = below * 8.0
             k2[:, hidden, :, 0] = mask
             both_places(q, k2, v, "hidden by %g, others at %d" % (mask, below))
+
+
+# keys shared out, by the plan in 2 to 40: wide kernels alone and in halves, joined by one and by sixteen groups of lanes
+SHARED = [(1, 1374, 9000, 16), (1, 2816, 8000, 16), (2, 440, 5000, 12), (20, 100, 2000, 4), (6, 65, 2000, 16), (1, 1374, 9000, 1),
+          (2, 700, 9000, 2), (1, 700, 20000, 1), (1, 20, 7001, 2)]
+
+
+@pytest.mark.parametrize("B, NQ, NK, H", SHARED)
+def test_shares_of_the_keys_count_by_their_sums(B, NQ, NK, H):
+    """The last share holds nearly all of a row's weight but begins with keys far below it, and is redone for another row's sake; the other
+    shares are not.  Their references say nothing about their sums."""
+    g = gen(42)
+    u = torch.sign(torch.randn(64, generator=g, device="cuda"))
+    q, k = bf16(g, B, NQ, H, 64, scale=0.1), bf16(g, B, NK, H, 64, scale=0.1)
+    v = bf16(g, B, NK, H, 64, scale=0.2)
+    q[..., 0], k[..., 0] = 8.0, -55.0
+    key, tiles = torch.arange(NK, device="cuda"), -(-NK // 64)
+    for shares in (2, 3, 4, 5, 10, 21, 40):
+        last = key >= 64 * (tiles * (shares - 1) // shares)
+        q2, k2, v2 = q.clone(), k.clone(), v.clone()
+        k2[:, last, :, 0] = -42.0
+        k2[:, last & (key % 64 < 32), :, 0] = -104.0
+        v2[:, last] += 1
+        v2[:, ~last] -= 1
+        spikes(q2, k2, u, last & (key % 64 == 63))
+        both_places(q2, k2, v2, "last of %d shares" % shares)
