@@ -262,8 +262,8 @@ __global__ __launch_bounds__(kFewThreads, kJ == 1 ? 4 : 2) void cross_few_kernel
     } else {
       const size_t at = partial_row(a, pairs, split, pair, r0 + row);
       *reinterpret_cast<f32x4*>(a.partial + at * kHeadDim + 4 * quad) = o;
-      if (quad == 0)
-        *reinterpret_cast<f32x2*>(partial_sums(a, pairs, plan.splits) + at * 2) = f32x2{hi > lo ? ref : -INFINITY, total};
+      // (-infinity: no keys, or none that weighs anything)
+      if (quad == 0) *reinterpret_cast<f32x2*>(partial_sums(a, pairs, plan.splits) + at * 2) = f32x2{top, total};
     }
   }
 }
@@ -587,7 +587,7 @@ __global__ __launch_bounds__(kJoinThreads) void cross_join_kernel(CrossArgs a, i
   const bool here = at < pairs * all && row < (uint32_t)queries * (uint32_t)a.group;
   float m = -INFINITY, l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  // another part of the sum, by its reference (-infinity: a split without keys, which adds nothing)
+  // another part of the sum, by its reference (-infinity: a split without keys that weigh anything, which adds nothing)
   auto add = [&](float m2, float l2, f32x4 o2) {
     const float now = fmaxf(m, m2), ref = now == -INFINITY ? 0.f : now;
     const float f = fast_exp2(m - ref), f2 = fast_exp2(m2 - ref);

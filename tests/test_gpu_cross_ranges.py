@@ -50,6 +50,7 @@ def judge(cross, got, q, k, v, what):
                 what, b, h, int(bad.sum()), float((off / tol)[~none].nan_to_num(1e9).max()))
             wl = torch.logsumexp(logit, -1)
             loff = (lse[b, h].double() - wl).abs()
+            assert bool((lse[b, h][wl == -math.inf] == -math.inf).all()), what
             there = ~none[:, 0]
             lbad = there & ~(loff <= pd[:, 0] + HALF + 2.0 ** -16 * (1 + wl.abs()))
             assert not bool(lbad.any()), "%s, element %d head %d: %d of lse off, worst %.3g" % (
@@ -124,3 +125,18 @@ def test_shares_of_the_keys_count_by_their_sums(B, NQ, NK, H):
         v2[:, ~last] -= 1
         spikes(q2, k2, u, last & (key % 64 == 63))
         both_places(q2, k2, v2, "last of %d shares" % shares)
+
+
+@pytest.mark.parametrize("B, NQ, NK, H", SHARED + [(1, 1, 20001, 2), (1, 30, 7001, 2), (1, 261, 16384, 2), (3, 5, 300, 2), (6, 512, 400, 64)])
+def test_keys_at_minus_infinity(B, NQ, NK, H):
+    """Keys whose logits are -infinity: whole shares of a sequence, all keys but one, and all of them, where O is no number and lse -infinity.
+    The others lie at ordinary logits, and far below zero."""
+    g = gen(43)
+    q, k, v = bf16(g, B, NQ, H, 64, scale=0.3), bf16(g, B, NK, H, 64, scale=0.3), bf16(g, B, NK, H, 64)
+    q[..., 0] = 8.0
+    for below in (0.0, -150.0):
+        for there in (slice(0, NK // 5), slice(4 * NK // 5, NK), slice(NK - 1, NK), slice(0, 1), slice(NK // 2, NK // 2 + 1), slice(0, 0)):
+            k2 = k.clone()
+            k2[..., 0] = -math.inf
+            k2[:, there, :, 0] = below
+            both_places(q, k2, v, "keys %s at %g" % (there, below))
