@@ -731,7 +731,7 @@ int make_append_args(const agg_cache* c, const agg_shape* shape, const agg_rope*
                       {counts, (uint64_t)c->B * 4}, {c->pages, table_bytes(c)}};
   for (const Bytes& o : out) {
     for (const Bytes& i : in)
-      if (!(in_place && o.p == Qr && i.p == Q) && overlap(o.p, o.n, i.p, i.n)) return AGG_ERR_SHAPE;
+      if (!(in_place && &o == &out[3] && &i == &in[0]) && overlap(o.p, o.n, i.p, i.n)) return AGG_ERR_SHAPE;  // (Qr over Q)
     for (const SeamNorm& n : r->norm)
       if (overlap_norm(o.p, o.n, n, kHeadDim)) return AGG_ERR_SHAPE;
     for (const Bytes& other : out)

@@ -317,3 +317,11 @@ def test_append_kernels_do_not_spill(tmp_path):
     found = list(metadata(text, "append_kernel"))
     assert len(found) == 8 and not [x for x in found if x[1]["vgpr_spill_count"]]
     assert "scratch_load" not in text and "scratch_store" not in text  # (scalar registers may spill, to lanes of a vector register)
+
+
+# ---- what only looks like an operand in place ------------------------------------------------------------
+def test_queries_in_place_are_nothing_else_of_the_call():
+    """Qr may be Q; that Q is also the keys, the values, positions, lengths or pages does not make these writable."""
+    for other in ("k", "v", "pos", "start", "counts", "pages"):
+        assert _append(HQ=2, qr=at(0), **{other: at(0)}) == S, other
+        assert _append(HQ=2, qr=at(0), **{other: at(0) + 16}) == S, other
