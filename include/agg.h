@@ -466,7 +466,8 @@ size_t agg_cross_workspace_bytes(const agg_cross* cross);
  * stride of Q), stride 0 meaning contiguous, otherwise a multiple of 8 and at least heads * 64.  Q, K, V: device bf16.
  * O: device bf16 [B, NQ, H, 64], contiguous; lse: device float32 [B, H, NQ] or NULL.  O and lse may overlap nothing else of
  * the call (AGG_ERR_SHAPE).  Logits and sums are float32; a key's probability is rounded to bf16 on its way into the second product, and
- * where a key head serves more than 32 queries the sum may be that of the rounded ones.
+ * where a key head serves more than 32 queries the sum may be that of the rounded ones.  Logits may lie anywhere; a row whose logits
+ * are all -infinity has O = NaN and lse = -infinity.  Sums of probability times value are float32 too: values beyond 2^100 may overflow them.
  */
 int agg_cross_attn_fwd(const agg_cross* cross, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
                        const void* V, int64_t v_stride, void* O, float* lse, void* workspace,

@@ -27,6 +27,7 @@ constexpr float kSumHi = 1.2379400392853803e27f;   // 2^90
 constexpr float kSumLo = 8.077935669463161e-28f;   // 2^-90
 constexpr float kLazy = 60.0f;  // general path: a unit may exceed the row's reference by 2^60
 constexpr float kUnitHi = 1.2676506002282294e30f;  // 2^100: a unit's row sum that forces a look
+constexpr float kUnitHiExact = 1024.0f;            // exact_logits: sooner, so that sums with values of up to 2^100 stay in float32's range
 
 union Frag {
   u32x4 u;
@@ -605,14 +606,14 @@ __device__ __forceinline__ void tile_steps(Wave<kQB, kJ>& w, const u32x4* __rest
     }
     __builtin_amdgcn_sched_barrier(0);
     if (kGen) {
-      // The unit's sums tell whether the reference still holds: a score more than 2^100 above it
+      // The unit's sums tell whether the reference still holds: a score more than 2^100 (exact_logits: 2^10) above it
       // cannot hide in them.  Rare, wavefront-uniform: raise the reference of the rows that need
       // it (the others keep theirs: shift 0, factor 1), scale what they have accumulated, and
       // redo the unit's probabilities (its scores are untouched until the next step).
       float all = unit_sum[0];
 #pragma unroll
       for (int j = 1; j < kJ; ++j) all += unit_sum[j];
-      if (__builtin_amdgcn_ballot_w64(!(all < kUnitHi)) != 0) {
+      if (__builtin_amdgcn_ballot_w64(!(all < (exact_logits(kSrc) ? kUnitHiExact : kUnitHi))) != 0) {
         f32x4 (&S)[2 * kJ] = w.S[qb];
         float ref[kJ];  // exact_logits: what the unit is taken relative to
 #pragma unroll

@@ -278,6 +278,12 @@ __global__ __launch_bounds__(kFewThreads, kJ == 1 ? 4 : 2) void cross_few_kernel
 // ---------------------------------------------------------------------------
 namespace {
 
+// Fast path: accumulators that may have overflowed; those that may have lost products below float32's range, where a row's probabilities are
+// as small as a sum below kSmallSum makes them
+constexpr float kOutHi = 1.329227995784916e36f;       // 2^120
+constexpr float kOutLo = 8.271806125530277e-25f;      // 2^-80
+constexpr float kSmallSum = 9.5367431640625e-7f;      // 2^-20
+
 // One workgroup's rows row_begin .. row_end - 1 of pair (b, hk) over its split's keys, by one of the two paths.  Returns false, without
 // storing anything, when the fast path met a row it cannot handle.  tiles: kTileLds elements of LDS per four wavefronts.
 template <int kSrc, bool kGen, int kQB, int kJ, int kMode = kAlone>
@@ -399,6 +405,20 @@ __device__ __forceinline__ bool attend_cross(const CrossArgs& p, const CrossPlan
     for (int j = 0; j < kJ; ++j) {
       l_fin[qb][j] = kGen ? quad_sum(w.la[qb][j]) : __shfl(w.L[qb][j][0], c);
       unsafe = unsafe || (group == 0 && (!(l_fin[qb][j] < kSumHi) || !(l_fin[qb][j] > kSumLo)));
+      if (!kGen) {
+        // sums inside the window say nothing of the values: probabilities of 2^80 overflow with values of 2^50, those of 2^-80
+        // vanish with values of 2^-50
+        float sum = 0.f, least = INFINITY;
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float size = fabsf(w.O[qb][j][dt][r]);
+            sum += size;
+            least = fminf(least, size);
+          }
+        unsafe = unsafe || (group == 0 && (!(sum < kOutHi) || (l_fin[qb][j] < kSmallSum && least < kOutLo)));
+      }
     }
   if (!kGen) {
     if (!done) return false;

@@ -140,3 +140,21 @@ def test_keys_at_minus_infinity(B, NQ, NK, H):
             k2[..., 0] = -math.inf
             k2[:, there, :, 0] = below
             both_places(q, k2, v, "keys %s at %g" % (there, below))
+
+
+@pytest.mark.parametrize("B, NQ, NK, H", KERNELS)
+def test_values_of_any_size(B, NQ, NK, H):
+    """Logits inside the fast path's window whose products with large or small values leave float32's, and rows that are redone relative to
+    keys far below the others."""
+    g = gen(44)
+    u = torch.sign(torch.randn(64, generator=g, device="cuda"))
+    q, k, v = bf16(g, B, NQ, H, 64, scale=0.3), bf16(g, B, NK, H, 64, scale=0.3), bf16(g, B, NK, H, 64)
+    q[..., 0] = 8.0
+    for at, size in ((45.0, 60), (45.0, -60), (-45.0, -90), (-45.0, 60), (0.0, 100), (0.0, -90)):
+        k[..., 0] = at
+        both_places(q, k, v * 2.0 ** size, "logits at %g, values 2^%d" % (at, size))
+    k[..., 0] = 0.0
+    k[:, torch.arange(NK, device="cuda") % 64 < 32, :, 0] = -45.0
+    spikes(q, k, u, [NK - 1])
+    for size in (60, 95, -90):
+        both_places(q, k, v * 2.0 ** size, "redone, values 2^%d" % size)
