@@ -468,6 +468,8 @@ size_t agg_cross_workspace_bytes(const agg_cross* cross);
  * the call (AGG_ERR_SHAPE).  Logits and sums are float32; a key's probability is rounded to bf16 on its way into the second product, and
  * where a key head serves more than 32 queries the sum may be that of the rounded ones.  Logits may lie anywhere; a row whose logits
  * are all -infinity has O = NaN and lse = -infinity.  Sums of probability times value are float32 too: values beyond 2^100 may overflow them.
+ * AGG_ERR_OVERFLOW, beside sizes beyond the index range: calls of more than 2^32 workgroups, and batch elements of more than 2^22
+ * workgroups of 128 or 256 rows (tens of GiB of queries each).
  */
 int agg_cross_attn_fwd(const agg_cross* cross, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
                        const void* V, int64_t v_stride, void* O, float* lse, void* workspace,
@@ -499,7 +501,7 @@ int agg_cache_bytes(const agg_cache* cache, size_t* bytes);
  * of cache->H (without Q it does not matter).  Rows before 0 and from 64*max_pages on are not stored.  lens (device int32 [B], may be
  * NULL) receives start[b] + counts[b], clamped to 0 .. 64*max_pages: what k_lens of the next call is.  Everything else in the
  * pools, and Qr of tokens that do not exist, is left as it was.  Two tokens of one call may not share a row.  No output may overlap
- * another operand of the call (AGG_ERR_SHAPE); lens may not be start.
+ * another operand of the call (AGG_ERR_SHAPE); lens may not be start.  More than 2^32 pieces of 32 rows: AGG_ERR_OVERFLOW.
  */
 int agg_cache_append(const agg_cache* cache, const agg_shape* shape, const agg_rope* rope, const agg_norm* q_norm,
                      const agg_norm* k_norm, const int32_t* pos, const void* Q, int64_t q_stride, const void* K,

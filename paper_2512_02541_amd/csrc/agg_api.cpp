@@ -574,6 +574,8 @@ int make_mx4_args(int64_t rows, int32_t N, int32_t K, const agg_mx4_linear* l, c
 }
 
 // ---- attention to keys of another length, the paged cache ----
+int launch_status(hipError_t e) { return e == hipSuccess ? AGG_OK : e == kTooManyGroups ? AGG_ERR_OVERFLOW : AGG_ERR_LAUNCH; }
+
 bool misaligned4(const void* p) { return ((uintptr_t)p & 3u) != 0; }
 
 // the sizes of a call, without its pointers
@@ -836,7 +838,7 @@ int agg_cross_attn_fwd(const agg_cross* cross, const void* Q, int64_t q_stride, 
   CrossArgs a;
   const int rc = make_cross_args(cross, nullptr, Q, q_stride, K, k_stride, V, v_stride, O, lse, workspace, workspace_bytes, &a);
   if (rc != AGG_OK || a.NQ == 0) return rc;
-  return launch_cross(a, (hipStream_t)hip_stream) == hipSuccess ? AGG_OK : AGG_ERR_LAUNCH;
+  return launch_status(launch_cross(a, (hipStream_t)hip_stream));
 }
 
 int agg_cache_bytes(const agg_cache* cache, size_t* bytes) {
@@ -855,7 +857,7 @@ int agg_cache_append(const agg_cache* cache, const agg_shape* shape, const agg_r
   const int rc = make_append_args(cache, shape, rope, q_norm, k_norm, pos, Q, q_stride, K, k_stride, V, v_stride, start, counts,
                                   lens, Qr, &a);
   if (rc != AGG_OK) return rc;
-  return launch_append(a, (hipStream_t)hip_stream) == hipSuccess ? AGG_OK : AGG_ERR_LAUNCH;
+  return launch_status(launch_append(a, (hipStream_t)hip_stream));
 }
 
 int agg_cache_attn_fwd(const agg_cache* cache, const agg_cross* cross, const void* Q, int64_t q_stride, void* O,
@@ -864,7 +866,7 @@ int agg_cache_attn_fwd(const agg_cache* cache, const agg_cross* cross, const voi
   CrossArgs a;
   const int rc = make_cross_args(cross, cache, Q, q_stride, nullptr, 0, nullptr, 0, O, lse, workspace, workspace_bytes, &a);
   if (rc != AGG_OK || a.NQ == 0) return rc;
-  return launch_cross(a, (hipStream_t)hip_stream) == hipSuccess ? AGG_OK : AGG_ERR_LAUNCH;
+  return launch_status(launch_cross(a, (hipStream_t)hip_stream));
 }
 
 // ---- one global-attention block --------------------------------------------------------

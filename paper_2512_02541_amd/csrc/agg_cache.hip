@@ -312,7 +312,7 @@ hipError_t launch_append(const AppendArgs& args, hipStream_t st) {
   a.parts = 1;
   while (a.parts < most && (int64_t)a.B * a.units * (a.parts + 1) <= kAtOnce) ++a.parts;
   a.items = (int64_t)a.B * a.units * a.parts;
-  if (a.items > 0xFFFFFFFFll) return hipErrorInvalidConfiguration;
+  if (a.items > 0xFFFFFFFFll) return kTooManyGroups;
   (void)hipGetLastError();
   if (few) launch_rows<16>(a, st);
   else launch_rows<32>(a, st);

@@ -671,7 +671,7 @@ size_t cross_partial_floats(int64_t B, int64_t NQ, int64_t NK, int64_t H, int64_
 template <bool kPaged>
 static hipError_t launch_few(const CrossArgs& a, const CrossPlan& p, int64_t pairs, hipStream_t st) {
   const int64_t groups = pairs * p.row_tiles * p.splits;
-  if (groups > 0xFFFFFFFFll) return hipErrorInvalidConfiguration;
+  if (groups > 0xFFFFFFFFll) return kTooManyGroups;
   constexpr int64_t kMost = 1 << 22;  // workgroups of a launch (kLaunchRows)
   for (int64_t first = 0; first < groups; first += kMost) {
     const uint32_t here = (uint32_t)(groups - first < kMost ? groups - first : kMost);
@@ -687,9 +687,9 @@ static hipError_t launch_wide(const CrossArgs& a, const CrossPlan& p, hipStream_
   // workgroups of a launch (kLaunchRows): beyond that parts of the batch are launches of their own, which share out nothing along the keys
   constexpr int64_t kMost = 1 << 22;
   const int64_t of_one = (int64_t)a.H_kv * p.row_tiles * p.splits;
-  if (of_one > kMost) return hipErrorInvalidConfiguration;
+  if (of_one > kMost) return kTooManyGroups;
   const int64_t step = a.B * of_one <= kMost ? a.B : kMost / of_one;
-  if (step < a.B && p.splits > 1) return hipErrorInvalidConfiguration;
+  if (step < a.B && p.splits > 1) return kTooManyGroups;
   for (int64_t b = 0; b < a.B; b += step) {
     WideArgs w = {a, p};
     w.a.B = (int32_t)(a.B - b < step ? a.B - b : step);

@@ -242,6 +242,8 @@ struct CrossArgs {
 };
 // whether the sequences of a call may have different lengths: 0: no, 2: of queries and of keys, 1: of one of them
 inline int cross_ragged(int32_t B, const int32_t* q_lens, const int32_t* k_lens) { return B > 1 ? (q_lens != nullptr) + (k_lens != nullptr) : 0; }
+// What the two launches below return, before anything is launched, for calls of more workgroups than they count.  (No launch returns it.)
+constexpr hipError_t kTooManyGroups = hipErrorNotSupported;
 // floats of workspace
 size_t cross_partial_floats(int64_t B, int64_t NQ, int64_t NK, int64_t H, int64_t H_kv, int ragged);
 hipError_t launch_cross(const CrossArgs& args, hipStream_t st);

@@ -325,3 +325,22 @@ def test_queries_in_place_are_nothing_else_of_the_call():
     for other in ("k", "v", "pos", "start", "counts", "pages"):
         assert _append(HQ=2, qr=at(0), **{other: at(0)}) == S, other
         assert _append(HQ=2, qr=at(0), **{other: at(0) + 16}) == S, other
+
+
+# ---- more workgroups than a call counts --------------------------------------------------------------------
+def test_calls_of_too_many_workgroups_are_sizes_beyond_the_index_range():
+    far = [1 << (48 + i) for i in range(5)] + [(1 << 47) + (i << 40) for i in range(8)]
+    # 2^22 wide workgroups of a batch element and some, rows in place and in pages
+    c = agg.make_cross(1, 2 ** 26 + 256, 1000, 16)
+    need = agg.agg_cross_workspace_bytes(c)
+    assert need == 0
+    assert _status(agg.agg_cross_attn_fwd, c, far[0], 0, far[1], 0, far[2], 0, far[3]) == O
+    cache = agg.agg_cache(100, 16, 64, 1, 16, far[5], far[6], far[7])
+    assert _status(agg.agg_cache_attn_fwd, cache, c, far[0], 0, far[3]) == O
+    # 2^32 workgroups of 32 rows: distances that the wide kernels do not reach
+    c = agg.make_cross(2 ** 20, 2 ** 19, 1, 1)
+    assert _status(agg.agg_cross_attn_fwd, c, far[0], 0, far[1], 2 ** 23 + 8, far[2], 2 ** 23 + 8, far[3]) == O
+    # 2^32 pieces of new tokens
+    cache = agg.agg_cache(100, 1, 64, 2 ** 31 - 1, 1, far[5], far[6], far[4])
+    shape = agg.make_shape(2 ** 31 - 1, 1, 1, 64, 0, 1, 64, 1, 1)
+    assert _status(agg.agg_cache_append, cache, shape, None, None, None, None, None, 0, far[1], 0, far[2], 0) == O
