@@ -222,9 +222,11 @@ def make_cross(B, NQ, NK, H, H_kv=None, D=64, scale=None, q_lens=None, k_lens=No
 
 
 def make_cache(Kc, Vc, pages, H, D=64, n_pages=None) -> agg_cache:
-    """pages: int32 [sequences, pages of each] on the device.  n_pages None: as many as the tensor Kc holds."""
+    """pages: int32 [sequences, pages of each] on the device.  n_pages None: as many as the tensors Kc and Vc both hold."""
     B, max_pages = (int(n) for n in pages.shape)
-    c = agg_cache(int(Kc.numel() // (H * 64 * 64) if n_pages is None else n_pages), int(H), int(D), B, max_pages,
+    if n_pages is None:
+        n_pages = min(Kc.numel(), Vc.numel()) // (H * 64 * 64)
+    c = agg_cache(int(n_pages), int(H), int(D), B, max_pages,
                   _ptr(Kc), _ptr(Vc), _ptr(pages))
     c.keep = (Kc, Vc, pages)
     return c

@@ -344,3 +344,11 @@ def test_calls_of_too_many_workgroups_are_sizes_beyond_the_index_range():
     cache = agg.agg_cache(100, 1, 64, 2 ** 31 - 1, 1, far[5], far[6], far[4])
     shape = agg.make_shape(2 ** 31 - 1, 1, 1, 64, 0, 1, 64, 1, 1)
     assert _status(agg.agg_cache_append, cache, shape, None, None, None, None, None, 0, far[1], 0, far[2], 0) == O
+
+
+# ---- the binding -------------------------------------------------------------------------------------------
+def test_a_cache_has_the_pages_that_both_pools_hold():
+    k, v = torch.zeros(5 * 2 * 4096, dtype=torch.bfloat16), torch.zeros(3 * 2 * 4096, dtype=torch.bfloat16)
+    pages = torch.zeros((1, 1), dtype=torch.int32)
+    assert agg.make_cache(k, v, pages, 2).n_pages == 3 and agg.make_cache(v, k, pages, 2).n_pages == 3
+    assert agg.make_cache(k, k, pages, 2).n_pages == 5 and agg.make_cache(k, v, pages, 2, n_pages=2).n_pages == 2
