@@ -95,7 +95,7 @@ __device__ __forceinline__ void turn8(float (&x)[8], const Channels& ch, int lan
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const int i = 2 * q + e;
-      const float turned = x[i] * cs[2 * e] + y[i] * cs[2 * e + 1];
+      const float turned = turn_channel(x[i], y[i], cs[2 * e], cs[2 * e + 1]);
       // by selection: an infinity times 0 is none of the other channels' business
       y[i] = (ch.other[i / 4] >> (8 * (i % 4))) & 0x80u ? turned : x[i];
     }

@@ -42,6 +42,9 @@ __device__ inline void load8(const float* p, int at, float other, float (&v)[8])
   }
 }
 
+// a channel turned with its other one; which product is rounded is said here, so that every kernel rounds the same
+__device__ inline float turn_channel(float x, float other, float cosine, float sine) { return fmaf(x, cosine, other * sine); }
+
 // the sum over eight neighbouring lanes, in all of them: two exchanges within four lanes, one between them
 __device__ inline float sum_of_8(float v) {
   v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xB1, 0xF, 0xF, true));   // lane ^ 1

@@ -162,7 +162,7 @@ __global__ __launch_bounds__(kRopeThreads, 4) void rope_kernel(RopeArgs a) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) y[i] = head[other[i]];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) y[i] = x[i] * cs[i / 2][i % 2 * 2] + y[i] * cs[i / 2][i % 2 * 2 + 1];
+          for (int i = 0; i < 8; ++i) y[i] = turn_channel(x[i], y[i], cs[i / 2][i % 2 * 2], cs[i / 2][i % 2 * 2 + 1]);
           if (all_turn) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] = y[i];

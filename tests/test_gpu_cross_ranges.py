@@ -15,10 +15,11 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import cache_oracle as orc
 from paper_2512_02541_amd import binding as agg
 from paper_2512_02541_amd import harness
 
-from test_gpu_cross import bf16, gen, pages_of, put, say
+from test_gpu_cross import bf16, gen, ints, norm_of, pages_of, put, same_bits, say
 
 pytestmark = pytest.mark.gpu
 
@@ -158,3 +159,26 @@ def test_values_of_any_size(B, NQ, NK, H):
     spikes(q, k, u, [NK - 1])
     for size in (60, 95, -90):
         both_places(q, k, v * 2.0 ** size, "redone, values 2^%d" % size)
+
+
+# ---- appending: the rotary call's numbers ---------------------------------------------------------------------
+@pytest.mark.parametrize("pairing", [agg.AGG_ROPE_SECTIONS, agg.AGG_ROPE_NEIGHBOURS, agg.AGG_ROPE_HEAD])
+@pytest.mark.parametrize("axes", [(0, 32, 32), (16, 24, 24), (20, 22, 14), (64, 0, 0)])
+@pytest.mark.parametrize("kind, frames", [("none", 2), ("layer", 1), ("rms", 16)])
+def test_appended_keys_and_queries_are_those_of_the_rotary_call(pairing, axes, kind, frames):
+    """To the bit, in pieces of 16 rows and of 32, wherever a channel's other one lies."""
+    say("as the rotary call", pairing, axes, kind)
+    g = gen(55)
+    H = 16
+    shape = agg.make_shape(1, frames, 37, 37, 5, H, 64, 1, 1)
+    T = shape.NQ
+    q, k, v = (bf16(g, 1, T, H, 64) for _ in "qkv")
+    rope, norm = agg.make_rope(pairing, *axes, base=1000.0, t0=3, patch0=1), norm_of(g, kind)[0]
+    pages, pool = pages_of(g, 1, -(-(T + 21) // 64))
+    pools = harness.make_pools(pool, H, "cuda")
+    qr = torch.empty_like(q)
+    agg.agg_cache_append(agg.make_cache(*pools, pages, H), shape, rope, norm, norm, None, q, 0, k, 0, v, 0, ints([21]), None, None, qr)
+    want = harness.rope_forward(shape, rope, q, k, norm, norm)
+    torch.cuda.synchronize()
+    assert same_bits(qr, want[0])
+    assert same_bits(orc.rows_of(pools[0], pages, orc.k_place)[:, 21:21 + T].contiguous(), want[1])
