@@ -352,3 +352,39 @@ def test_a_cache_has_the_pages_that_both_pools_hold():
     pages = torch.zeros((1, 1), dtype=torch.int32)
     assert agg.make_cache(k, v, pages, 2).n_pages == 3 and agg.make_cache(v, k, pages, 2).n_pages == 3
     assert agg.make_cache(k, k, pages, 2).n_pages == 5 and agg.make_cache(k, v, pages, 2, n_pages=2).n_pages == 2
+
+
+# ---- the plan of ragged calls --------------------------------------------------------------------------------
+def test_plans_of_queries_and_keys_that_end_early(plan):
+    sizes = [(pairs, rows, keys, 2, fits, paged) for pairs in (1, 3, 16, 100, 4096, 2 ** 22, 2 ** 23 + 5, 2 ** 31 - 1)
+             for rows in (1, 16, 17, 33, 64, 65, 257, 400, 1374, 10992, 2 ** 30)
+             for keys in (0, 1, 31, 64, 1000, 20000, 137400, 2 ** 31 - 600) for fits in (0, 1) for paged in (0, 1)]
+    for (pairs, rows, keys, _, fits, _), (width, tail, halves, row_tiles, splits) in zip(sizes, plan(sizes)):
+        assert row_tiles * width >= rows > (row_tiles - 1) * width
+        assert width in (16, 32, 128, 256) and (fits or width < 128) and (width < 128 or rows > 32)
+        assert tail in (0, 128, 192) and (tail == 0 or (width == 256 and 0 < rows % 256 <= tail))
+        assert not halves or width == 128
+        assert 1 <= splits <= 64 and (splits == 1 or keys // splits >= (192 if width >= 128 else 1))
+        assert splits == 1 or pairs * row_tiles * splits <= 4096
+
+
+def test_ragged_sizes_reach_their_kernels(plan):
+    import test_gpu_cross_ranges as gpu
+
+    for ragged in (1, 2):
+        for paged in (0, 1):
+            asked = [(B * H, NQ, NK, ragged, 1, paged) for B, NQ, NK, H, queries in gpu.RAGGED if queries == ragged - 1]
+            got = {(width, tail, halves, splits > 1) for width, tail, halves, _, splits in plan(asked)}
+            want = {(w, t, 0, s) for w, t in ((32, 0), (128, 0), (256, 0), (256, 128), (256, 192)) for s in (False, True)} | {(128, 0, 1, False)}
+            assert got >= want, (ragged, paged, want - got)
+
+
+def test_far_and_hidden_sizes_reach_every_wide_kernel(plan):
+    """The sizes whose logits lie far apart run every wide kernel, out of pages and in place, with and without shared out keys."""
+    import test_gpu_cross_ranges as gpu
+
+    for paged in (0, 1):
+        got = {(width, tail, halves, splits > 1)
+               for width, tail, halves, _, splits in plan([(B * H, NQ, NK, 0, 1, paged) for B, NQ, NK, H in gpu.KERNELS])}
+        want = {(w, t, h, s) for w, t, h in ((128, 0, 0), (128, 0, 1), (256, 0, 0), (256, 128, 0), (256, 192, 0)) for s in (False, True)}
+        assert got >= want, (paged, want - got)

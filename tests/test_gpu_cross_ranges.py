@@ -19,7 +19,7 @@ from oracle import cache_oracle as orc
 from paper_2512_02541_amd import binding as agg
 from paper_2512_02541_amd import harness
 
-from test_gpu_cross import bf16, gen, ints, norm_of, pages_of, put, same_bits, say
+from test_gpu_cross import bf16, both, check, gen, ints, norm_of, pages_of, put, same_bits, say
 
 pytestmark = pytest.mark.gpu
 
@@ -182,3 +182,88 @@ def test_appended_keys_and_queries_are_those_of_the_rotary_call(pairing, axes, k
     torch.cuda.synchronize()
     assert same_bits(qr, want[0])
     assert same_bits(orc.rows_of(pools[0], pages, orc.k_place)[:, 21:21 + T].contiguous(), want[1])
+
+
+# ---- paths that only far or many things take ----------------------------------------------------------------
+# ragged calls of every kernel, with and without shared out keys: B, NQ, NK, H, and whether queries end early too
+RAGGED = [(2, 40, 100, 1, 0), (2, 40, 1000, 1, 0), (3, 65, 100, 32, 0), (2, 65, 5000, 16, 0), (3, 65, 9000, 4, 0), (5, 100, 1000, 16, 0),
+          (3, 65, 1000, 32, 0), (2, 2816, 100, 32, 0), (5, 2816, 9000, 8, 0), (20, 520, 100, 16, 0), (5, 1374, 14000, 16, 0), (8, 700, 100, 32, 0),
+          (5, 130, 14000, 32, 0), (2, 40, 100, 1, 1), (2, 40, 1000, 1, 1), (5, 100, 100, 16, 1), (5, 65, 5000, 8, 1), (5, 100, 9000, 2, 1),
+          (3, 100, 1000, 32, 1), (5, 100, 1000, 16, 1), (5, 2816, 100, 16, 1), (5, 1000, 9000, 32, 1), (20, 520, 100, 32, 1),
+          (8, 1374, 14000, 16, 1), (20, 700, 100, 16, 1), (8, 130, 14000, 32, 1)]
+
+
+@pytest.mark.parametrize("B, NQ, NK, H, queries", RAGGED)
+def test_ragged_calls_of_every_kernel(B, NQ, NK, H, queries):
+    k_lens = ([NK, NK // 2, 0, NK - 1, 1, 65, NK + 3, -1] * 3)[:B]
+    q_lens = ([NQ, NQ - 1, NQ, 1, NQ // 2, 0, NQ, 33] * 3)[:B] if queries else None
+    both(B, NQ, NK, H, seed=51, q_lens=q_lens, k_lens=k_lens)
+
+
+@pytest.mark.parametrize("NQ", [1, 20, 64, 300])
+def test_rows_further_apart_than_wide_kernels_reach(NQ):
+    say("far rows", NQ)
+    g = gen(52)
+    H, NK, stride = 2, 3, (1 << 23) + 8
+    q, k, v = bf16(g, 2, NQ, H, 64), bf16(g, 2, NK, H, 64), bf16(g, 2, NK, H, 64)
+    wide = torch.full((2 * NK * stride,), math.nan, dtype=torch.bfloat16, device="cuda")
+    rows, beside = (torch.as_strided(wide, (2 * NK, H * 64), (stride, 1), at) for at in (0, H * 64))
+    rows.copy_(k.view(2 * NK, -1))
+    beside.copy_(v.view(2 * NK, -1))
+    cross = agg.make_cross(2, NQ, NK, H, k_lens=ints([3, 2]))
+    check(cross, harness.cross_forward(cross, q, wide, wide[H * 64:], 0, stride, stride), q, k, v, None, [3, 2], "far rows")
+
+
+def test_a_batch_of_more_wide_workgroups_than_a_launch_takes():
+    """2^22 sequences and five: two launches, in place and out of pages."""
+    g = gen(53)
+    B, H, NK = (1 << 22) + 5, 33, 2
+    q = torch.randn((B, 1, H, 64), generator=g, device="cuda", dtype=torch.bfloat16)
+    k, v = (torch.randn((B, NK, 1, 64), generator=g, device="cuda", dtype=torch.bfloat16) for _ in "kv")
+    ql = torch.randint(0, 2, (B,), generator=g, device="cuda", dtype=torch.int32)
+    kl = torch.randint(0, NK + 1, (B,), generator=g, device="cuda", dtype=torch.int32)
+    seen = torch.cat((torch.arange(20, device="cuda"), torch.arange((1 << 22) - 20, B, device="cuda"),
+                      torch.randint(0, B, (100,), generator=g, device="cuda")))
+    cross = agg.make_cross(B, 1, NK, H, 1, q_lens=ql, k_lens=kl)
+    assert agg.agg_cross_workspace_bytes(cross) == 0
+    pages = torch.randint(0, 50, (B, 1), generator=g, device="cuda", dtype=torch.int32)
+    pools = [torch.randn((50, 1, 4096), generator=g, device="cuda", dtype=torch.bfloat16) for _ in "kv"]
+    o, lse = torch.empty_like(q), torch.empty((B, H, 1), device="cuda")
+    some = agg.make_cross(len(seen), 1, NK, H, 1)
+    for paged in (False, True):
+        say("many wide workgroups", paged)
+        o.view(torch.int16).fill_(0x7FC1)
+        lse.fill_(math.nan)
+        if paged:
+            agg.agg_cache_attn_fwd(agg.make_cache(*pools, pages, 1), cross, q, 0, o, lse)
+            ks, vs = (orc.rows_of(p, pages[seen], place)[:, :NK] for p, place in zip(pools, (orc.k_place, orc.v_place)))
+        else:
+            agg.agg_cross_attn_fwd(cross, q, 0, k, 0, v, 0, o, lse)
+            ks, vs = k[seen], v[seen]
+        check(some, (o[seen], lse[seen]), q[seen], ks, vs, ql[seen].tolist(), kl[seen].tolist(), "paged" if paged else "in place")
+        for h in (0, H - 1):
+            assert torch.equal(torch.isnan(o[:, 0, h, 5]), ql == 0) and torch.equal(torch.isnan(lse[:, h, 0]), ql == 0)
+
+
+def test_more_pieces_of_new_tokens_than_a_launch_has_workgroups():
+    """2^19 sequences and three of one token each, whose rows fill pages that they share: 2^20 pieces and six."""
+    say("many pieces")
+    g = gen(54)
+    B = (1 << 19) + 3
+    shape = agg.make_shape(B, 1, 1, 1, 0, 1, 64, 1, 1)
+    k, v = bf16(g, B, 1, 1, 64), bf16(g, B, 1, 1, 64)
+    number = torch.arange(B, device="cuda", dtype=torch.int32)
+    pages, start = (number // 64).view(B, 1).contiguous(), number % 64
+    pools = harness.make_pools(B // 64 + 1, 1, "cuda")
+    lens = harness._buf((B,), torch.int32, "cuda", "lens")
+    pos = torch.randint(0, 1000, (B, 1, 3), generator=g, device="cuda", dtype=torch.int32)
+    rope, norm = agg.make_rope(agg.AGG_ROPE_SECTIONS, 0, 32, 32), agg.make_norm(agg.AGG_NORM_RMS, 1e-5)
+    agg.agg_cache_append(agg.make_cache(*pools, pages, 1), shape, rope, None, norm, pos, None, 0, k, 0, v, 0, start, None, lens)
+    _, turned = harness.rope_forward(shape, rope, None, k, None, norm, pos)
+    torch.cuda.synchronize()
+    assert torch.equal(lens, start + 1)
+    table = torch.arange(B // 64 + 1, device="cuda", dtype=torch.int32).view(1, -1)
+    for p, t, place in zip(pools, (turned, v), (orc.k_place, orc.v_place)):
+        rows = orc.rows_of(p, table, place)[0]
+        assert same_bits(rows[:B].contiguous(), t.view(B, 1, 64))
+        assert bool((rows[B:].contiguous().view(torch.int16) == 0x7FC1).all())
