@@ -126,7 +126,7 @@ struct Wave {
   f32x4 S[kQB][2 * kJ];    // [qb][kJ kt + j]: score tiles in flight; key = row_key(4 G + r) + 8 kt
   f32x4 L[kQB][kJ];        // [qb][j]: fast path: element 0 of the lanes G = 0 is the row sum, kept by the matrix core
   float la[kQB][kJ];       // [qb][j]: general path: this lane's part of the row sum
-  float mref[kQB][kJ];     // general path: the row's reference (base-2 logit; exact_logits: -infinity where it has none yet)
+  float mref[kQB][kJ];     // general path: the row's reference (base-2 logit; exact_logits: plain product, -infinity where there is none yet)
   Frag a[4];               // [2 kt + h]: K fragments of the block whose scores are being computed
   Frag v[4];               // [dt]: V fragments of the block whose P V is being accumulated
   Frag P[kJ];              // [j]: probabilities of the previous unit
@@ -171,8 +171,9 @@ __device__ __forceinline__ void exp_unit_sum(const f32x4 (&S)[2 * kJ], Frag (&P)
       }
 }
 
-// General path of exact_logits: the scores are plain products and become base-2 logits relative to each row's reference in one
-// multiply-add.  The difference is rounded after it is taken: a reference far above or far below these scores costs them no digits.
+// General path of exact_logits: the scores and each row's reference are plain products, whose difference becomes a base-2 logit.  A
+// reference far above or far below the scores costs them no digits, and one of their own is never below them: of references that are
+// rounded products with l2, 10^10 is 512 off, and a multiply-add with it makes 2^512 of the row's largest probability.
 template <int kJ>
 __device__ __forceinline__ void exp_unit_relative(const f32x4 (&S)[2 * kJ], Frag (&P)[kJ], float (&l)[kJ], float l2, const float (&ref)[kJ]) {
 #pragma unroll
@@ -181,8 +182,8 @@ __device__ __forceinline__ void exp_unit_relative(const f32x4 (&S)[2 * kJ], Frag
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int j = 0; j < kJ; ++j) {
-        const float e0 = fast_exp2(fmaf(S[kJ * kt + j][2 * i], l2, -ref[j]));
-        const float e1 = fast_exp2(fmaf(S[kJ * kt + j][2 * i + 1], l2, -ref[j]));
+        const float e0 = fast_exp2((S[kJ * kt + j][2 * i] - ref[j]) * l2);
+        const float e1 = fast_exp2((S[kJ * kt + j][2 * i + 1] - ref[j]) * l2);
         P[j].u[2 * kt + i] = pack_bf16(e0, e1);
         l[j] += e0;
         l[j] += e1;
@@ -633,9 +634,9 @@ __device__ __forceinline__ void tile_steps(Wave<kQB, kJ>& w, const u32x4* __rest
           if (exact_logits(kSrc)) {
             // A row without a reference gets here by itself: relative to -infinity its sum is infinite or no number.  It has none
             // as long as all its logits are -infinity, whose probabilities are 0 relative to anything.
-            w.mref[qb][j] = fmaxf(old, mx * w.l2 + kAboveExact);
+            w.mref[qb][j] = fmaxf(old, mx + fminf(kAboveExact * __builtin_amdgcn_rcpf(w.l2), 1e30f));
             ref[j] = w.mref[qb][j] == -INFINITY ? 0.f : w.mref[qb][j];
-            f = fast_exp2(old - ref[j]);
+            f = fast_exp2((old - ref[j]) * w.l2);
           } else {
             if (mx > kLazy) w.mref[qb][j] = old + mx;
             const float d = w.mref[qb][j] - old;

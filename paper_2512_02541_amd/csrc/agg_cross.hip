@@ -138,7 +138,7 @@ __global__ __launch_bounds__(kFewThreads, kJ == 1 ? 4 : 2) void cross_few_kernel
   };
 
   f32x4 O[kJ][4];
-  float m[kJ], l[kJ];  // m: largest logit so far, base 2; l: this lane's part of the sum
+  float m[kJ], l[kJ];  // m: largest score so far, a plain product (exp_unit_relative); l: this lane's part of the sum
 #pragma unroll
   for (int j = 0; j < kJ; ++j) {
     m[j] = -INFINITY;
@@ -192,9 +192,9 @@ __global__ __launch_bounds__(kFewThreads, kJ == 1 ? 4 : 2) void cross_few_kernel
       for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
         for (int r = 0; r < 4; ++r) top = fmaxf(top, S[kJ * kt + j][r]);
-      const float now = fmaxf(m[j], quad_max(top) * a.scale2);
+      const float now = fmaxf(m[j], quad_max(top));
       const float ref = now == -INFINITY ? 0.f : now;  // (logits may be -infinity)
-      const float f = fast_exp2(m[j] - ref);
+      const float f = fast_exp2((m[j] - ref) * a.scale2);
       m[j] = now;
       l[j] *= f;
 #pragma unroll
@@ -203,8 +203,8 @@ __global__ __launch_bounds__(kFewThreads, kJ == 1 ? 4 : 2) void cross_few_kernel
       for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const float e0 = fast_exp2(fmaf(S[kJ * kt + j][2 * i], a.scale2, -ref));
-          const float e1 = fast_exp2(fmaf(S[kJ * kt + j][2 * i + 1], a.scale2, -ref));
+          const float e0 = fast_exp2((S[kJ * kt + j][2 * i] - ref) * a.scale2);
+          const float e1 = fast_exp2((S[kJ * kt + j][2 * i + 1] - ref) * a.scale2);
           P[j].u[2 * kt + i] = pack_bf16(e0, e1);
           l[j] += e0 + e1;
         }
@@ -253,17 +253,17 @@ __global__ __launch_bounds__(kFewThreads, kJ == 1 ? 4 : 2) void cross_few_kernel
 #pragma unroll
     for (int w = 0; w < kW; ++w) {
       const f32x2 s = *reinterpret_cast<const f32x2*>(sums + (w * 16 * kJ + row) * 2);
-      const float f = fast_exp2(s[0] - ref);
+      const float f = fast_exp2((s[0] - ref) * a.scale2);
       total += s[1] * f;
       o += *reinterpret_cast<const f32x4*>(lds + (w * 16 * kJ + row) * kRowFloats + 4 * quad) * f;
     }
     if (plan.splits == 1) {
-      store_row(a, b, hk, r0 + row, quad, ref, total, o, n == 0);
+      store_row(a, b, hk, r0 + row, quad, ref * a.scale2, total, o, n == 0);
     } else {
       const size_t at = partial_row(a, pairs, split, pair, r0 + row);
       *reinterpret_cast<f32x4*>(a.partial + at * kHeadDim + 4 * quad) = o;
       // (-infinity: no keys, or none that weighs anything)
-      if (quad == 0) *reinterpret_cast<f32x2*>(partial_sums(a, pairs, plan.splits) + at * 2) = f32x2{top, total};
+      if (quad == 0) *reinterpret_cast<f32x2*>(partial_sums(a, pairs, plan.splits) + at * 2) = f32x2{top * a.scale2, total};
     }
   }
 }
@@ -451,7 +451,7 @@ __device__ __forceinline__ bool attend_cross(const CrossArgs& p, const CrossPlan
         }
         if (eG == 0)
           *reinterpret_cast<f32x2*>(partial_sums(p, pairs, plan.splits) + at * 2) =
-              f32x2{(kGen ? w.mref[qb][j] : 0.f) + (float)e, ldexpf(l_fin[qb][j], -e)};
+              f32x2{(kGen ? w.mref[qb][j] * p.scale2 : 0.f) + (float)e, ldexpf(l_fin[qb][j], -e)};
       }
     return true;
   }
@@ -468,7 +468,7 @@ __device__ __forceinline__ bool attend_cross(const CrossArgs& p, const CrossPlan
         *reinterpret_cast<u32x2*>(epi + (16 * j + ec) * kEpiStride + 16 * dt + 4 * eG) = pack4(w.O[qb][j][dt] * inv);
       if (p.lse && eG == 0 && r0 + 16 * j + ec < row_end) {
         const RowPlace at = row_place(p, hk, r0 + 16 * j + ec);
-        p.lse[((int64_t)b * p.H + at.head) * p.NQ + at.q] = ((kGen ? w.mref[qb][j] : 0.f) + log2f(l)) * kLn2;
+        p.lse[((int64_t)b * p.H + at.head) * p.NQ + at.q] = ((kGen ? w.mref[qb][j] * p.scale2 : 0.f) + log2f(l)) * kLn2;
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");

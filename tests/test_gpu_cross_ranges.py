@@ -161,6 +161,24 @@ def test_values_of_any_size(B, NQ, NK, H):
         both_places(q, k, v * 2.0 ** size, "redone, values 2^%d" % size)
 
 
+@pytest.mark.parametrize("B, NQ, NK, H", KERNELS)
+def test_logits_of_any_size(B, NQ, NK, H):
+    """Logits of up to 10^37, where a step of float32 is many powers of two of a probability: of the first half of every tile, of all keys, and
+    of all keys but the last, of either sign; rows that are redone among them."""
+    g = gen(45)
+    u = torch.sign(torch.randn(64, generator=g, device="cuda"))
+    q, k, v = bf16(g, B, NQ, H, 64), bf16(g, B, NK, H, 64, scale=0.5), bf16(g, B, NK, H, 64)
+    q[..., 0], k[..., 0] = 1.0, 0.0
+    spikes(q, k, u, [NK - 1])
+    key = torch.arange(NK, device="cuda")
+    lowest = torch.finfo(torch.bfloat16).min
+    for size in (-8e7, -8e10, -8e20, lowest, 8e10, -lowest):
+        for where, there in (("half of every tile", (key % 64 < 32) & (key < NK - 1)), ("all", key >= 0), ("all but the last", key < NK - 1)):
+            k2 = k.clone()
+            k2[:, there, :, 0] = size
+            both_places(q, k2, v, "%s at %g" % (where, size))
+
+
 # ---- appending: the rotary call's numbers ---------------------------------------------------------------------
 @pytest.mark.parametrize("pairing", [agg.AGG_ROPE_SECTIONS, agg.AGG_ROPE_NEIGHBOURS, agg.AGG_ROPE_HEAD])
 @pytest.mark.parametrize("axes", [(0, 32, 32), (16, 24, 24), (20, 22, 14), (64, 0, 0)])
