@@ -28,8 +28,8 @@ constexpr float kSumLo = 8.077935669463161e-28f;   // 2^-90
 constexpr float kLazy = 60.0f;  // general path: a unit may exceed the row's reference by 2^60
 constexpr float kUnitHi = 1.2676506002282294e30f;  // 2^100: a unit's row sum that forces a look
 // exact_logits: a look at 2^10, so that sums with values of up to 2^100 stay in float32's range, and references 20 above (base 2) the
-// largest logit so far, so that it is not taken for every rise.  (Redone calls, us, logits of +-20 / 40 / 100, 512 queries to each of 24 frames: 184 /
-// 185 / 187 without the 20 and 172 / 176 / 183 with it; 168 / 163 / 171 with a look at 2^100, which overflows with values of 2^50.)
+// largest logit so far, so that it is not taken for every rise.  (Redone calls, us, logits of +-20 / 40 / 100, 512 queries to each of 24
+// frames: 191 / 195 / 199 without the 20, 177 / 183 / 192 with it; 168 / 166 / 175 with a look at 2^100, which overflows with values of 2^50.)
 constexpr float kUnitHiExact = 1024.0f;
 constexpr float kAboveExact = 20.0f;
 

@@ -8,6 +8,8 @@ channels (S* that of the row's largest logit) and v its value:
        ones, 2^-8 more; float32 steps behind it 2^-12: sum of p (2^-7 + 2^-12 + d) |v|, by the sum |O| sum of p d, by the result's rounding 2^-8 |O|
   lse  sum of p d; 2^-16 (1 + |lse|) for the logarithm and the base; 2^-8 where the sum is that of rounded probabilities
 Keys whose probability is zero in float64 count as nothing, whatever their logit.
+That is first order in d.  Where d reaches 1/2 for a key within d of the row's largest logit (logits of 10^5 and more), float32 cannot tell which
+keys weigh most: O has to be some mean of values, no further from the right one than twice the largest, and lse within the largest d.
 """
 import math
 
@@ -38,11 +40,16 @@ def judge(cross, got, q, k, v, what):
             logit = (qh @ kh.t().contiguous()) * scale
             p = torch.softmax(logit, -1)
             S = (qh.abs() @ kh.abs().t().contiguous()) * scale
-            S = torch.where(p > 0, S, torch.zeros_like(S))
-            d = DOT * (S + S.gather(1, logit.argmax(1, keepdim=True)))
+            top = logit.argmax(1, keepdim=True)
+            d = DOT * (S + S.gather(1, top))
+            near = logit.gather(1, top) - logit <= d
+            most = torch.where(near & torch.isfinite(d), d, torch.zeros_like(d)).amax(1, keepdim=True)
+            d = torch.where(p > 0, d, torch.zeros_like(d))
             want = p @ vh
             pd = (p * d).sum(1, keepdim=True)
             tol = (p * (2 * HALF + 2.0 ** -12 + d)) @ vh.abs() + want.abs() * (pd + HALF)
+            pd = torch.where(most < 0.5, pd, most)
+            tol = torch.where(most < 0.5, tol, (2 + HALF) * vh.abs().amax(0))
             off = (o[b, :, h].double() - want).abs()
             none = torch.isnan(want)
             assert bool(torch.isnan(o[b, :, h])[none].all()), what + ": numbers where there are none"
